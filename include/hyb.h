@@ -293,6 +293,84 @@ int hyb_mmdit_forward(const hyb_mmdit_desc* desc, const hyb_mmdit_weights* weigh
                       int txt_pre_only_last, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Packed batches: the tokens of several requests of different sizes (resolutions, clip lengths, prompts) one after the other
+ * along ONE token axis, without padding, so that a launch serves all of them.  `offsets` arrays are device int[n + 1]: request
+ * (sequence) s owns the rows offsets[s] .. offsets[s + 1] - 1; they do not decrease.  Offsets are read by the kernels only: a
+ * captured graph replays on whatever they hold by then.  Offsets outside 0 .. the number of rows are taken as the nearest
+ * of these, so that no call reads or writes outside its tensors.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Offsets, request index and (time, height, width) position of every token of a packed batch from the requests' sizes.
+ * shapes: device int[requests][4] = (frames, height, width, text tokens); negative numbers count as 0.  A request has frames x height x
+ * width image tokens, width running fastest, and then its text tokens.  offsets: device int[requests + 1], at most `capacity` each: rows that
+ * do not fit are cut off.  request, positions: device int[capacity], int[capacity][3], or NULL (skipped); rows behind
+ * the last request are left as they are.  Text tokens stand at (0, 0, 0), or with text_after != 0 at
+ * m + j on all three axes for text token j, m = max(frames, height, width). */
+int hyb_packed_layout(const int* shapes, int requests, int capacity, int text_after,
+                      int* offsets, int* request, int* positions, void* stream);
+
+/* Which features of a head form a pair that is rotated together; pairs are numbered 0 .. R / 2 - 1, R = the sum of axis_dims. */
+typedef enum {
+    HYB_ROTARY_NEIGHBOURS = 0,   /* pair j = features 2 j, 2 j + 1 */
+    HYB_ROTARY_HALVES = 1        /* pair j = features j, j + R / 2 */
+} hyb_rotary_pairs;
+
+#define HYB_ROTARY_MAX_AXES 4
+typedef struct {
+    int tokens;
+    int q_heads, k_heads;                            /* at most 512; either may be 0: nothing is done for that tensor */
+    int head_dim;                                    /* multiple of 16, at most 256 */
+    int axes;                                        /* 1 .. 4 position numbers per token */
+    int axis_dims[HYB_ROTARY_MAX_AXES];              /* features of each axis: even, > 0; their sum R <= head_dim (HYB_ROTARY_HALVES: R % 16 == 0) */
+    float axis_scale[HYB_ROTARY_MAX_AXES];           /* positions of the axis are multiplied by this (0 means 1) */
+    float theta;                                     /* > 0 */
+    hyb_rotary_pairs pairs;
+    int inverse;                                     /* non-zero: by the negative angle, which is the transpose: the gradient of the forward call */
+    float q_scale;                                   /* every feature of q is multiplied by this before its one rounding (0 means 1) */
+    hyb_dtype dtype;
+    size_t q_stride, k_stride, q_out_stride, k_out_stride;   /* elements from one token to the next, multiples of 16 bytes, >= heads * head_dim */
+} hyb_rotary_desc;
+
+/* Rotary positions with several axes on queries and keys.  The first axis_dims[0] / 2 pairs of a head turn with the token's first position number, the
+ * next axis_dims[1] / 2 with the second, and so on: pair j of axis a turns by positions[token][a] * axis_scale[a] * theta^(-2 j / axis_dims[a])
+ * (j counted inside the axis), (x, y) -> (x cos - y sin, x sin + y cos).  Features R .. head_dim - 1 are not turned.
+ * positions: device int[tokens][axes].  q, q_out: device, head h of token t at t * stride + h * head_dim elements (heads adjacent; a slice of the
+ * output of a joint q / k / v projection is such a tensor); the same for k, k_out.  q_out may be q and k_out may be k, then with the same stride;
+ * otherwise outputs must not share elements with inputs.
+ * Angles are formed in fp64, sines and cosines in fp32 (to 2^-22), products and sums in fp32, one rounding at the end.
+ * (q_scale = scale * log2(e) makes the queries of hyb_packed_attention's prescaled form.) */
+int hyb_rotary(const hyb_rotary_desc* desc, const int* positions, const void* q, void* q_out, const void* k, void* k_out, void* stream);
+
+typedef struct {
+    int sequences;
+    int total_q, total_k;                            /* rows of q and o, rows of k and v */
+    int max_q, max_k;                                /* most queries / keys of one sequence, 0: unknown.  They choose the way to the result (splits), not the result */
+    int q_heads, k_heads;                            /* q_heads % k_heads == 0: query head h reads key head h / (q_heads / k_heads) */
+    int head_dim;                                    /* 64 or 128 */
+    float scale;                                     /* <= 0 means 1 / sqrt(head_dim) */
+    int causal;                                      /* non-zero: query i of a sequence of n_q queries and n_k keys sees the keys j <= i + n_k - n_q */
+    int prescaled;                                   /* non-zero: q holds q * scale * log2(e) (as for hyb_joint_attention_prescaled); `scale` is not used */
+    hyb_dtype dtype;
+    size_t q_token_stride, q_head_stride;            /* elements; multiples of 16 bytes, less than 2^23 elements from token to token */
+    size_t k_token_stride, k_head_stride;
+    size_t v_token_stride, v_head_stride;
+    size_t o_token_stride, o_head_stride;
+} hyb_packed_attention_desc;
+
+/* o = softmax(q k^T * scale) v for every sequence of a packed batch over its own keys: joint attention of images of different sizes with their
+ * text, whole prompts (causal), new tokens at the end of longer caches (causal with n_q < n_k), single queries.
+ * offsets_q, offsets_k: device int[sequences + 1].  q, o: device, feature i of head h of row t at t * token_stride + h * head_stride + i; k, v
+ * likewise with k_heads heads.  Token-major and head-major tensors and slices of joint projections are all of this form.
+ * A query that sees no key (its sequence has none, or causal with n_q > n_k) gets zeros.  What a key holds that a query does not see, infinities and
+ * NaN among it, does not reach that query.  Rows of o that belong to no sequence are left as they are.
+ * Calls with few query rows cut the keys into parts that other workgroups take and merge the unnormalised partial results in a second kernel, in a
+ * fixed order: deterministic, but the number of parts, which follows from the descriptor alone, may decide last bits.
+ * workspace: device, >= hyb_packed_attention_workspace_bytes(desc) (0: may be NULL), contents irrelevant; calls that overlap in time need one each. */
+int hyb_packed_attention(const hyb_packed_attention_desc* desc, const void* q, const void* k, const void* v, void* o,
+                         const int* offsets_q, const int* offsets_k, void* workspace, size_t workspace_bytes, void* stream);
+size_t hyb_packed_attention_workspace_bytes(const hyb_packed_attention_desc* desc);
+
+/* ------------------------------------------------------------------------------------------
  * Second denoiser shape (the U-Net family of Sec. 5's setup): one transformer block of an
  * SDXL-shaped attention stage on token-major activations.
  * ---------------------------------------------------------------------------------------- */

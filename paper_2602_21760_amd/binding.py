@@ -77,6 +77,24 @@ class SdxlBlockWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in SDXL_WEIGHT_FIELDS]
 
 
+HYB_ROTARY_NEIGHBOURS, HYB_ROTARY_HALVES = 0, 1
+HYB_ROTARY_MAX_AXES = 4
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int), ("head_dim", C.c_int), ("axes", C.c_int),
+                ("axis_dims", C.c_int * HYB_ROTARY_MAX_AXES), ("axis_scale", C.c_float * HYB_ROTARY_MAX_AXES), ("theta", C.c_float), ("pairs", C.c_int),
+                ("inverse", C.c_int), ("q_scale", C.c_float), ("dtype", C.c_int), ("q_stride", C.c_size_t), ("k_stride", C.c_size_t),
+                ("q_out_stride", C.c_size_t), ("k_out_stride", C.c_size_t)]
+
+
+class PackedAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("sequences", "total_q", "total_k", "max_q", "max_k", "q_heads", "k_heads", "head_dim")] + \
+               [("scale", C.c_float), ("causal", C.c_int), ("prescaled", C.c_int), ("dtype", C.c_int)] + \
+               [(n, C.c_size_t) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride",
+                                          "o_token_stride", "o_head_stride")]
+
+
 HYB_SWITCH_MAX_STEPS = 1024
 
 
@@ -112,6 +130,10 @@ SIGNATURES = {
     "hyb_patchify": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
     "hyb_unpatchify": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp]),
     "hyb_convert": (_i, [_vp, _vp, _sz, _i, _vp]),
+    "hyb_packed_layout": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp]),
+    "hyb_rotary": (_i, [C.POINTER(RotaryDesc), _vp, _vp, _vp, _vp, _vp, _vp]),
+    "hyb_packed_attention": (_i, [C.POINTER(PackedAttentionDesc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "hyb_packed_attention_workspace_bytes": (_sz, [C.POINTER(PackedAttentionDesc)]),
     "hyb_groupnorm": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _f, _vp, _sz, _vp]),
     "hyb_groupnorm_workspace_bytes": (_sz, [_i, _i]),
     "hyb_layernorm_affine": (_i, [_vp, _vp, _vp, _vp, _i, _i, _f, _i, _vp]),
@@ -400,6 +422,131 @@ def hyb_unpatchify(tokens, latent, p):
 def hyb_convert(src, out):
     _check(lib().hyb_convert(_p(src, torch.float32), _p(out), src.numel(), _dt(out), _stream()))
     return out
+
+
+def _here(*tensors):
+    """The tensors (None among them) live on the current device, whose stream the call goes to."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensor on %s, but the current device is cuda:%d" % (t.device, device))
+
+
+def hyb_packed_layout(shapes, offsets, request=None, positions=None, text_after=False):
+    """shapes: int32[requests, 4] = (frames, height, width, text tokens); offsets: int32[requests + 1]; request: int32[rows], positions: int32[rows, 3],
+    or None; rows is the capacity."""
+    if shapes.dim() != 2 or shapes.shape[1] != 4 or offsets.dim() != 1 or offsets.shape[0] != shapes.shape[0] + 1:
+        raise ValueError("shapes must be [requests, 4] and offsets [requests + 1]")
+    if (request is not None and request.dim() != 1) or (positions is not None and (positions.dim() != 2 or positions.shape[1] != 3)):
+        raise ValueError("request must be [rows] and positions [rows, 3]")
+    rows = {t.shape[0] for t in (request, positions) if t is not None}
+    if len(rows) > 1:
+        raise ValueError("request and positions must have the same number of rows")
+    args = _p(shapes, torch.int32), _p(offsets, torch.int32), _p(request, torch.int32), _p(positions, torch.int32)
+    _here(shapes, offsets, request, positions)
+    # (offsets alone: nothing is cut off)
+    _check(lib().hyb_packed_layout(args[0], shapes.shape[0], rows.pop() if rows else 0x7fffffff, bool(text_after), args[1], args[2], args[3], _stream()))
+    return offsets
+
+
+def _head_strides(t, name):
+    """(token stride, head stride) of a [tokens, heads, head_dim] tensor whose features are adjacent, in elements; the stride of an axis of one element
+    says nothing and is taken as if the tensor were contiguous."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+        raise ValueError("%s must be [tokens, heads, head_dim] with adjacent features" % name)
+    head = t.stride(1) if t.shape[1] != 1 else t.shape[2]
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * head, t.shape[1] * t.shape[2]), head
+
+
+def _like(t):
+    return t.shape, t.stride(), t.dtype
+
+
+def _checked(desc, tensors):
+    """Device pointers of the tensors of a call (None -> NULL); they must be laid out as those that the descriptor was made from."""
+    device, out = torch._C._cuda_getDevice(), []
+    for t, like in zip(tensors, desc.like):
+        if like is None:
+            out.append(None)
+            continue
+        if t is None or (t.shape, t.stride(), t.dtype) != like:
+            raise ValueError("a tensor differs in shape, strides or type from the one that the descriptor was made from")
+        if t.get_device() != device:
+            raise ValueError("tensor on %s, but the current device is cuda:%d" % (t.device, device))
+        out.append(t.data_ptr())
+    return out
+
+
+def rotary_desc(q, k, axis_dims, theta=10000.0, pairs=HYB_ROTARY_NEIGHBOURS, axis_scale=None, q_scale=1.0, inverse=False, q_out=None, k_out=None):
+    """Descriptor of hyb_rotary for q, k: [tokens, heads, head_dim] views with adjacent heads (k may be None); q_out, k_out: where the results go if
+    not in place."""
+    axes = len(axis_dims)
+    if not 1 <= axes <= HYB_ROTARY_MAX_AXES or len(axis_scale or axis_dims) != axes:
+        raise ValueError("axis_dims and axis_scale must have 1 to %d entries" % HYB_ROTARY_MAX_AXES)
+    if q_scale == 0.0 or (axis_scale is not None and 0.0 in axis_scale):
+        raise ValueError("scales must not be 0")
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens, heads, head_dim]")
+    strides = []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        for y in (x, x if out is None else out):
+            if y is None:
+                strides.append(0)
+                continue
+            if x is None or y.shape != x.shape or y.dtype != q.dtype or y.shape[0] != q.shape[0] or y.shape[2] != q.shape[2]:
+                raise ValueError("%s and %s_out must have the same shape, and the tokens, head_dim and type of q" % (name, name))
+            token, head = _head_strides(y, name)
+            if head != y.shape[2]:
+                raise ValueError("the heads of %s must be adjacent" % name)
+            strides.append(token)
+    desc = RotaryDesc(q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], axes, (C.c_int * 4)(*axis_dims), (C.c_float * 4)(*(axis_scale or ())),
+                      theta, pairs, int(inverse), q_scale, _dt(q), strides[0], strides[2], strides[1], strides[3])
+    desc.like = _like(q), k if k is None else _like(k), _like(q if q_out is None else q_out), k if k is None else _like(k if k_out is None else k_out)
+    return desc
+
+
+def hyb_rotary(desc, positions, q, k=None, q_out=None, k_out=None):
+    """positions: int32[tokens, axes]; q, k, q_out, k_out as desc was made (None: in place)."""
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    if positions.shape != (desc.tokens, desc.axes):
+        raise ValueError("positions must be [%d, %d]" % (desc.tokens, desc.axes))
+    p = _p(positions, torch.int32)
+    _here(positions)
+    pq, pk, pqo, pko = _checked(desc, (q, k, q_out, k_out))
+    _check(lib().hyb_rotary(C.byref(desc), p, pq, pqo, pk, pko, _stream()))
+    return q_out, k_out
+
+
+def packed_attention_desc(q, k, v, o, offsets_q, max_q=0, max_k=0, causal=False, scale=0.0, prescaled=False):
+    """Descriptor of hyb_packed_attention for q, o: [rows, q_heads, head_dim] and k, v: [rows, k_heads, head_dim] (views with any strides between tokens
+    and between heads, features adjacent); offsets_q: int32[sequences + 1]; max_q, max_k: most queries / keys of a sequence if known."""
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape != o.shape or q.shape[2] != k.shape[2]:
+        raise ValueError("q, o: [rows, q_heads, head_dim], k, v: [rows, k_heads, head_dim]")
+    if not q.dtype == k.dtype == v.dtype == o.dtype:
+        raise TypeError("q, k, v and o must be of one type")
+    if offsets_q.dim() != 1 or offsets_q.shape[0] < 1:
+        raise ValueError("offsets must be [sequences + 1]")
+    strides = [s for t, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o")) for s in _head_strides(t, n)]
+    desc = PackedAttentionDesc(offsets_q.shape[0] - 1, q.shape[0], k.shape[0], max_q, max_k, q.shape[1], k.shape[1], q.shape[2], scale, int(causal), int(prescaled),
+                               _dt(q), *strides)
+    desc.like = _like(q), _like(k), _like(v), _like(o)
+    return desc
+
+
+def hyb_packed_attention_workspace_bytes(desc):
+    return lib().hyb_packed_attention_workspace_bytes(C.byref(desc))
+
+
+def hyb_packed_attention(desc, q, k, v, o, offsets_q, offsets_k, workspace=None):
+    """q, k, v, o as desc was made; offsets_q, offsets_k: int32[sequences + 1]; workspace: torch.uint8 tensor of hyb_packed_attention_workspace_bytes(desc),
+    or None if that is 0."""
+    if offsets_q.shape != (desc.sequences + 1,) or offsets_k.shape != offsets_q.shape:
+        raise ValueError("offsets must be [%d]" % (desc.sequences + 1))
+    cq, ck, ws = _p(offsets_q, torch.int32), _p(offsets_k, torch.int32), _p(workspace)
+    _here(offsets_q, offsets_k, workspace)
+    pq, pk, pv, po = _checked(desc, (q, k, v, o))
+    _check(lib().hyb_packed_attention(C.byref(desc), pq, pk, pv, po, cq, ck, ws, _nbytes(workspace), _stream()))
+    return o
 
 
 def hyb_trace_enable(on):

@@ -1,0 +1,353 @@
+// fp32 attention over packed batches on the fp32 matrix cores (reference precision), the merge of cut keys for both types, and the entry point.
+//
+// As attention_f32.hip: a workgroup of 4 waves owns 32 rows (head_dim 128: 16) of one (sequence, key head) and splits the KEYS: wave w takes the 32-key
+// tiles w, w + 4, ... with a running maximum and normaliser of its own; the four partial results are merged in LDS in a fixed order.  Operands go
+// straight from memory (L2) to registers.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: a 16-byte load gives a lane 4 features of its key
+// for 4 MFMAs, and register i of the exponentiated S^T is the B operand of the MFMA over the keys 4 q4 + i, with rows 4 q4 + i of V as the A operand.
+#include "packed_attention.h"
+
+namespace {
+
+constexpr int BKV = 32;
+constexpr int WAVES = 4;
+
+// e^x for x <= 0 to 1.5 ulp: 2^n 2^f with n = x log2(e) rounded and f the rest, log2(e) in two parts; NaN stays NaN.
+__device__ __forceinline__ float exp_neg(float x) {
+    x = x < -200.f ? -200.f : x;
+    const float n = rintf(x * 1.44269502162933349609375f);
+    const float f = fmaf(x, 1.92596299112661746887e-8f, fmaf(x, 1.44269502162933349609375f, -n));
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+}
+
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
+    constexpr int BQ = packed_rows_f32(D), QT = BQ / 16, DT = D / 16, VH = D / 64;
+    __shared__ float part_o[WAVES][QT][DT][4][64];   // [wave][row tile][feature tile][register][lane]
+    __shared__ float part_ml[WAVES][QT][2][16];      // [wave][row tile][maximum, normaliser][row]
+    const PackedUnit u = packed_unit<BQ>(a);
+    if (u.rows == 0) return;
+    const int lane = threadIdx.x % 64, l16 = lane % 16, q4 = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const char* kp = static_cast<const char*>(a.k) + (size_t)u.k0 * a.k_token + (size_t)u.head * a.k_head;
+    const char* vp = static_cast<const char*>(a.v) + (size_t)u.k0 * a.v_token + (size_t)u.head * a.v_head;
+
+    f32x4 q[QT][DT];     // [row tile][16-feature step]
+    int last[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        const int row = u.row0 + min(qt * 16 + l16, u.rows - 1), t = row / a.group;
+        last[qt] = packed_last_key(a, u, t);
+        const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + row - t * a.group) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < DT; s++) q[qt][s] = *reinterpret_cast<const f32x4*>(qp + 64 * s + 16 * q4);
+    }
+    const int block_min = packed_last_key(a, u, u.row0 / a.group), block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
+    const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;
+    const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
+    const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
+
+    float m[QT], l[QT];
+    f32x4 o[DT][QT];     // [feature tile][row tile]
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        m[qt] = -__builtin_inff();
+        l[qt] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int t = t_begin + wave; t < t_end; t += WAVES) {
+        const int key0 = t * BKV;
+        f32x4 k[2][DT], v[2][4][VH];     // K: [key tile][16-feature step]; V: [key tile][row 4 q4 + i][64 features]
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++) {
+            const char* row = kp + (size_t)min(key0 + kt * 16 + l16, u.n_k - 1) * a.k_token + 16 * q4;
+#pragma unroll
+            for (int s = 0; s < DT; s++) k[kt][s] = *reinterpret_cast<const f32x4*>(row + 64 * s);
+        }
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const char* row = vp + (size_t)min(key0 + kt * 16 + 4 * q4 + i, u.n_k - 1) * a.v_token + 16 * l16;
+#pragma unroll
+                for (int h = 0; h < VH; h++) v[kt][i][h] = *reinterpret_cast<const f32x4*>(row + 256 * h);
+            }
+        f32x4 s[2][QT];      // [key tile][row tile]: keys 16 kt + 4 q4 + i
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) s[kt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < DT; st++)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                    for (int qt = 0; qt < QT; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][st][j], q[qt][st][j], s[kt][qt], 0, 0, 0);
+        const bool masked = key0 + BKV - 1 > block_min;
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            const int seen = last[qt] - key0 - 4 * q4;      // keys 16 kt + i > seen are hidden
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) s[kt][qt][i] = kt * 16 + i > seen ? -__builtin_inff() : s[kt][qt][i] * a.scale;
+            float mx = fmaxf(fmaxf(fmaxf(s[0][qt][0], s[0][qt][1]), fmaxf(s[0][qt][2], s[0][qt][3])),
+                             fmaxf(fmaxf(s[1][qt][0], s[1][qt][1]), fmaxf(s[1][qt][2], s[1][qt][3])));
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m[qt], mx);
+            const float corr = m[qt] == m_new ? 1.f : exp_neg(m[qt] - m_new);   // first tile: exp(-inf) = 0
+            m[qt] = m_new;
+            l[qt] *= corr;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) o[dt][qt] *= corr;
+            const float ref = m_new == -__builtin_inff() ? 0.f : m_new;          // only hidden keys so far: all probabilities 0
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    s[kt][qt][i] = exp_neg(s[kt][qt][i] - ref);
+                    l[qt] += s[kt][qt][i];
+                }
+        }
+        // a probability of 0 does not keep an infinity or NaN of a hidden key's value out of the MFMA: such values are added to the rows that see them by hand
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int h = 0; h < VH; h++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) odd |= not_finite(v[kt][i][h][e]);
+            odd = __any(odd);
+        }
+        if (odd) {
+#pragma unroll 1
+            for (int key = key0; key < min(key0 + BKV, u.n_k); key++) {
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float x = *reinterpret_cast<const float*>(vp + (size_t)key * a.v_token + 4 * ((dt / 4) * 64 + 16 * q4 + 4 * i + dt % 4));
+#pragma unroll
+                        for (int qt = 0; qt < QT; qt++)
+                            if (not_finite(x) && key <= last[qt]) o[dt][qt][i] += x;
+                    }
+            }
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int h = 0; h < VH; h++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) v[kt][i][h][e] = not_finite(v[kt][i][h][e]) ? 0.f : v[kt][i][h][e];
+        }
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+                    for (int qt = 0; qt < QT; qt++) o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[kt][i][dt / 4][dt % 4], s[kt][qt][i], o[dt][qt], 0, 0, 0);
+    }
+
+    // merge of the waves: row = sum_p o_p e^(m_p - M) / sum_p l_p e^(m_p - M), p in order
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        l[qt] += __shfl_xor(l[qt], 16, 64);
+        l[qt] += __shfl_xor(l[qt], 32, 64);
+        if (q4 == 0) {
+            part_ml[wave][qt][0][l16] = m[qt];
+            part_ml[wave][qt][1][l16] = l[qt];
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) part_o[wave][qt][dt][i][lane] = o[dt][qt][i];
+    }
+    __syncthreads();
+    // wave w finishes register w of every tile: features 64 h + 16 q4 + 4 w .. + 3 of row l16
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        if (qt * 16 + l16 >= u.rows) continue;
+        float m_all = part_ml[0][qt][0][l16];
+#pragma unroll
+        for (int p = 1; p < WAVES; p++) m_all = fmaxf(m_all, part_ml[p][qt][0][l16]);
+        float l_all = 0.f;
+        f32x4 r[VH];
+#pragma unroll
+        for (int h = 0; h < VH; h++) r[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < WAVES; p++) {
+            const float mp = part_ml[p][qt][0][l16], lp = part_ml[p][qt][1][l16];
+            if (lp == 0.f) continue;     // a wave without keys for this row counts nothing
+            const float w = mp == m_all ? 1.f : exp_neg(mp - m_all);
+            l_all = fmaf(lp, w, l_all);
+#pragma unroll
+            for (int h = 0; h < VH; h++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) r[h][e] = fmaf(part_o[p][qt][4 * h + e][wave][lane], w, r[h][e]);
+        }
+        const int row = u.row0 + qt * 16 + l16, tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+        if (a.parts > 1) {
+            const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
+            if (q4 == 0 && wave == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{m_all, l_all};
+#pragma unroll
+            for (int h = 0; h < VH; h++) *reinterpret_cast<f32x4*>(a.part + at * D + 64 * h + 16 * q4 + 4 * wave) = r[h];
+            continue;
+        }
+        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 4 * (16 * q4 + 4 * wave);
+#pragma unroll
+        for (int h = 0; h < VH; h++) *reinterpret_cast<f32x4*>(op + 256 * h) = l_all == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : r[h] / l_all;
+    }
+}
+
+// Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
+// (fp32: e^(m_p - M)), M = max m_p over the parts with keys, parts in index order.  One thread per 4 features.  Bound by the partial results it reads.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, float c) {
+    const int parts = a.parts;
+    a.parts = 1;                          // a workgroup per (block, head)
+    const PackedUnit u = packed_unit<ROWS>(a);
+    const float* ml0 = a.part + (size_t)a.total_q * a.q_heads * parts * D;
+    for (int i = threadIdx.x; i < u.rows * (D / 4); i += 256) {
+        const int row = u.row0 + i / (D / 4), f = i % (D / 4) * 4;
+        const int tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+        const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * parts;
+        const f32x2* ml = reinterpret_cast<const f32x2*>(ml0) + at;
+        float m_all = -__builtin_inff();
+        for (int p = 0; p < parts; p++)
+            if (ml[p][1] != 0.f) m_all = fmaxf(m_all, ml[p][0]);
+        float l = 0.f;
+        f32x4 r = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < parts; p++) {
+            if (ml[p][1] == 0.f) continue;
+            const float d = ml[p][0] - m_all;
+            const float w = ml[p][0] == m_all ? 1.f : sizeof(T) == 4 ? exp_neg(d) : __builtin_amdgcn_exp2f(d * c);
+            l = fmaf(ml[p][1], w, l);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + (at + p) * D + f);
+#pragma unroll
+            for (int e = 0; e < 4; e++) r[e] = fmaf(v[e], w, r[e]);
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        T* op = reinterpret_cast<T*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head) + f;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(op) = r * inv;
+        else *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16_t)(r[0] * inv), (bf16_t)(r[1] * inv), (bf16_t)(r[2] * inv), (bf16_t)(r[3] * inv)};
+    }
+}
+
+template <typename T, int D, int ROWS>
+int launch_merge(PackedAttnArgs a, hipStream_t st) {
+    const float c = a.prescaled ? 1.f : a.scale * 1.4426950408889634f;
+    PackedAttnArgs whole = a;
+    whole.parts = 1;
+    HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D, ROWS>), packed_grid(whole), dim3(256), 0, st, a, c);
+    return hyb_check_launch("packed_attention_merge");
+}
+
+// How the keys are cut.  A launch whose row blocks would leave most of the chip idle (single tokens, the end of a long prompt) takes `parts` workgroups per
+// block, enough for every CU to hold its share, of at least 256 keys each.  max_k == 0: the keys of all sequences bound one sequence's.
+void choose_parts(PackedAttnArgs& a, int max_k, int head_dim, hyb_dtype dtype) {
+    a.parts = 1;
+    a.part_keys = 0;
+    const long long units = (long long)a.blocks * a.k_heads, slots = (long long)hyb_cu_count() * (dtype == HYB_BF16 && head_dim == 64 ? 4 : 2);
+    const int keys = max_k > 0 && max_k < a.total_k ? max_k : a.total_k;
+    if (units == 0 || units * 2 > slots || keys <= 512) return;
+    long long parts = slots / units;
+    int len = (int)((keys + parts - 1) / parts);
+    len = (len + 63) / 64 * 64;
+    if (len < 256) len = 256;
+    a.parts = (keys + len - 1) / len;
+    a.part_keys = len;
+}
+
+int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttnArgs& a) {
+    HYB_REQUIRE(desc != nullptr, HYB_ERR_NULL, "%s: argument 'desc' is NULL", who);
+    const hyb_packed_attention_desc& d = *desc;
+    HYB_ARG_DTYPE(who, d.dtype);
+    HYB_REQUIRE(d.sequences >= 0 && d.total_q >= 0 && d.total_k >= 0 && d.max_q >= 0 && d.max_k >= 0, HYB_ERR_SHAPE, "%s: negative size", who);
+    HYB_REQUIRE(d.head_dim == 64 || d.head_dim == 128, HYB_ERR_SHAPE, "%s: head_dim %d is not supported (only 64 and 128)", who, d.head_dim);
+    HYB_REQUIRE(d.q_heads > 0 && d.k_heads > 0 && d.q_heads <= 65535 && d.q_heads % d.k_heads == 0, HYB_ERR_SHAPE, "%s: %d query heads are no multiple of %d key heads", who, d.q_heads, d.k_heads);
+    const size_t es = hyb_dtype_size(d.dtype), vec = 16 / es;
+    const size_t strides[8] = {d.q_token_stride, d.q_head_stride, d.k_token_stride, d.k_head_stride, d.v_token_stride, d.v_head_stride, d.o_token_stride, d.o_head_stride};
+    for (size_t s : strides) {
+        HYB_REQUIRE(s % vec == 0, HYB_ERR_ALIGN, "%s: a stride of %zu elements is not a multiple of 16 bytes", who, s);
+        HYB_REQUIRE(s < ((size_t)1 << 40), HYB_ERR_SHAPE, "%s: a stride of %zu elements is too large", who, s);
+    }
+    for (int i = 0; i < 8; i += 2) HYB_REQUIRE(strides[i] < ((size_t)1 << 23), HYB_ERR_SHAPE, "%s: a token stride of %zu elements is not below 2^23", who, strides[i]);
+    a = {};
+    a.sequences = d.sequences; a.total_q = d.total_q; a.total_k = d.total_k;
+    a.q_heads = d.q_heads; a.k_heads = d.k_heads; a.group = d.q_heads / d.k_heads;
+    a.scale = d.scale > 0.f ? d.scale : (d.head_dim == 64 ? 0.125f : 0.08838834764831845f);
+    a.causal = d.causal != 0; a.prescaled = d.prescaled != 0;
+    if (a.prescaled && d.dtype == HYB_F32) {      // the fp32 kernel exponentiates scale x score in base e
+        a.scale = 0.6931471805599453f;
+        a.prescaled = 0;
+    }
+    a.q_token = d.q_token_stride * es; a.q_head = d.q_head_stride * es; a.k_token = d.k_token_stride * es; a.k_head = d.k_head_stride * es;
+    a.v_token = d.v_token_stride * es; a.v_head = d.v_head_stride * es; a.o_token = d.o_token_stride * es; a.o_head = d.o_head_stride * es;
+    const int rows = d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim);
+    HYB_REQUIRE((long long)d.total_q * a.group < (1ll << 31) && packed_blocks(a, rows) * a.k_heads < (1ll << 27), HYB_ERR_SHAPE, "%s: too many queries (%d rows of %d heads)", who, d.total_q, d.q_heads);
+    a.blocks = (int)packed_blocks(a, rows);
+    a.xcd_heads = d.k_heads % 8 == 0 ? 8 : d.k_heads % 4 == 0 ? 4 : d.k_heads % 2 == 0 ? 2 : 1;
+    a.xcd_share = 8 / a.xcd_heads;
+    choose_parts(a, d.max_k, d.head_dim, d.dtype);
+    return HYB_OK;
+}
+
+size_t part_bytes(const PackedAttnArgs& a, int head_dim) {
+    return a.parts > 1 ? hyb_align_up(packed_part_floats(a.total_q, a.q_heads, a.parts, head_dim) * sizeof(float), 256) : 0;
+}
+
+}  // namespace
+
+int hyb_launch_packed_attention_f32(const PackedAttnArgs& a, int head_dim, hipStream_t st) {
+    HybTraceScope trace("packed_attention_f32", "byte", 8.0 * head_dim * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
+    if (head_dim == 64) hipLaunchKernelGGL(packed_attention_f32_kernel<64>, packed_grid(a), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(packed_attention_f32_kernel<128>, packed_grid(a), dim3(256), 0, st, a);
+    return hyb_check_launch("packed_attention_f32");
+}
+
+extern "C" size_t hyb_packed_attention_workspace_bytes(const hyb_packed_attention_desc* desc) {
+    PackedAttnArgs a;
+    if (fill_args("hyb_packed_attention_workspace_bytes", desc, a) != HYB_OK) return 0;
+    return part_bytes(a, desc->head_dim);
+}
+
+extern "C" int hyb_packed_attention(const hyb_packed_attention_desc* desc, const void* q, const void* k, const void* v, void* o,
+                                    const int* offsets_q, const int* offsets_k, void* workspace, size_t workspace_bytes, void* stream) {
+    PackedAttnArgs a;
+    int rc = fill_args("hyb_packed_attention", desc, a);
+    if (rc) return rc;
+    const hyb_packed_attention_desc& d = *desc;
+    if (d.sequences == 0 || d.total_q == 0) return HYB_OK;
+    HYB_CHECK_PTR(q); HYB_CHECK_PTR(o); HYB_CHECK_PTR(offsets_q); HYB_CHECK_PTR(offsets_k);
+    HYB_CHECK_ALIGN(q); HYB_CHECK_ALIGN(o); HYB_CHECK_ALIGN(offsets_q); HYB_CHECK_ALIGN(offsets_k);
+    if (d.total_k > 0) { HYB_CHECK_PTR(k); HYB_CHECK_PTR(v); }
+    HYB_CHECK_ALIGN(k); HYB_CHECK_ALIGN(v);
+    const size_t heads = (size_t)d.q_heads, row = (size_t)d.head_dim;
+    HYB_REQUIRE((d.o_head_stride >= row && d.o_token_stride >= (heads - 1) * d.o_head_stride + row) ||
+                    (d.o_token_stride >= row && d.o_head_stride >= ((size_t)d.total_q - 1) * d.o_token_stride + row),
+                HYB_ERR_SHAPE, "hyb_packed_attention: the strides of o let its rows overlap");
+    const size_t need = part_bytes(a, d.head_dim);
+    if (need > 0) {
+        HYB_CHECK_PTR(workspace); HYB_CHECK_ALIGN(workspace);
+        HYB_REQUIRE(workspace_bytes >= need, HYB_ERR_WORKSPACE, "hyb_packed_attention: workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
+        a.part = static_cast<float*>(workspace);
+    }
+    a.q = q; a.k = k; a.v = v; a.o = o; a.offsets_q = offsets_q; a.offsets_k = offsets_k;
+    const hipStream_t st = (hipStream_t)stream;
+    rc = d.dtype == HYB_BF16 ? hyb_launch_packed_attention_mfma(a, d.head_dim, st) : hyb_launch_packed_attention_f32(a, d.head_dim, st);
+    if (rc || a.parts == 1) return rc;
+    if (d.dtype == HYB_BF16) return d.head_dim == 64 ? launch_merge<bf16_t, 64, kPackedRowsMfma>(a, st) : launch_merge<bf16_t, 128, kPackedRowsMfma>(a, st);
+    return d.head_dim == 64 ? launch_merge<float, 64, packed_rows_f32(64)>(a, st) : launch_merge<float, 128, packed_rows_f32(128)>(a, st);
+}

@@ -1,0 +1,321 @@
+// Attention over packed batches for gfx950, bf16 operands, head_dim 64 or 128: a streaming softmax over 64-key tiles, scores never stored.
+//
+// A workgroup of 4 waves owns 128 rows (queries x heads of a group, see packed_attention.h) of one (sequence, key head), each wave 32 of
+// them (two tiles of 16).  Keys and values come 64 at a time through double-buffered LDS tiles by 16-byte direct-to-LDS copies, rows unpadded
+// with their 16-byte slots XOR-swizzled.  Both contractions run on v_mfma_f32_16x16x32_bf16 in transposed form, S^T = K Q^T and
+// O^T += V^T P^T: lane (l16 = lane % 16, q4 = lane / 16) of an accumulator tile holds column l16 and rows 4 q4 .. 4 q4 + 3, so all scores of a
+// lane belong to ONE row per 16-row tile, row sums are per-lane scalars plus two exchanges at the end, and the exponentiated scores of key tiles
+// 2 s and 2 s + 1, rounded to bf16, are the B operand of the second contraction as they lie (the order of a contraction's index does not
+// matter as long as both operands agree: k = 4 q4 + i of key tile 2 s, then of 2 s + 1).
+//
+// Softmax in fp32, base 2.  A workgroup first sums 2^(c score) without a reference maximum (c = scale x log2 e; 1 for queries that carry it);
+// that is the softmax as long as every row's sum lies in [2^-64, 2^64].  If a row's does not, the workgroup starts over with a running maximum.
+// Probabilities are rounded to bf16 for the second contraction and the normaliser is the sum of the rounded ones.
+//
+// Masks: the last key that a row sees is one number per row (causal, or the end of the sequence); only tiles in which a wave's rows differ from
+// "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA, so such a tile is
+// searched for them first, and if there are any (never in sane data) they are zeroed in the fragments and added to the rows that see them.
+#include "packed_attention.h"
+
+#include <type_traits>
+
+namespace {
+
+constexpr int BQ = kPackedRowsMfma;
+constexpr int BKV = 64;
+constexpr float RESCALE_LOG2 = 8.0f;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef void __attribute__((address_space(3)))* lptr_t;
+
+template <int D> __device__ __forceinline__ int swz(int r) {
+    // 128-byte rows: see attention_mfma.hip.  256-byte rows cover all banks: 16 rows (8 for the transposing reads, which take 32 bytes of a row) go to different slots.
+    return D == 64 ? (r & 6) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+__device__ __forceinline__ bool not_finite(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
+
+template <int D, bool PRE>
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(PackedAttnArgs a) {
+    constexpr int ROWB = D * 2, TILE_BYTES = BKV * ROWB, SLOTS = ROWB / 16;
+    constexpr int CHUNK_ROWS = 1024 / ROWB, CHUNKS = BKV / CHUNK_ROWS / 4;      // rows of a 1 KB copy; copies per wave, operand and tile
+    constexpr int KS = D / 32, DT = D / 16;
+    // [buffer][K tile | V tile]
+    __shared__ __attribute__((aligned(256))) unsigned char smem[2][2 * TILE_BYTES];
+
+    const PackedUnit u = packed_unit<BQ>(a);
+    if (u.rows == 0) return;
+    const int tid = threadIdx.x, lane = tid % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int l16 = lane % 16, q4 = lane / 16;
+    const int kq = (q4 >> 1) | ((q4 & 1) << 1);      // which 8 of a step's 32 features the lane holds (lanes i and i + 32 take neighbouring slots)
+
+    // the lane's rows, one per 16-row tile (rows behind the block's last are copies of it, never stored)
+    int last[2];                                     // last key that the row sees
+    bf16x8 qf[2][KS];
+#pragma unroll
+    for (int qt = 0; qt < 2; qt++) {
+        const int row = u.row0 + min(wave * 32 + qt * 16 + l16, u.rows - 1);
+        const int t = row / a.group, g = row - t * a.group;
+        last[qt] = packed_last_key(a, u, t);
+        const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + g) * a.q_head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) qf[qt][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 64 + kq * 16);
+    }
+    // the wave's rows see at least the keys 0 .. wave_min and at most 0 .. wave_max, the block's rows at most 0 .. block_max
+    const int wave_min = packed_last_key(a, u, (u.row0 + min(wave * 32, u.rows - 1)) / a.group);
+    const bool active = wave * 32 < u.rows;
+    const int wave_max = active ? packed_last_key(a, u, (u.row0 + min(wave * 32 + 31, u.rows - 1)) / a.group) : -1;
+    const int block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
+
+    const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;                    // (block_max == -1: no tile)
+    const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
+    const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
+
+    // Tile copy: lane i of a 1 KB chunk fills slot i % SLOTS of row i / SLOTS with feature vector slot ^ swz(row).  The tile's first row is in the
+    // resource (64-bit), so an offset never exceeds a tile.  Only the ragged last tile has its rows clamped.
+    const char* kp = static_cast<const char*>(a.k) + (size_t)u.k0 * a.k_token + (size_t)u.head * a.k_head;
+    const char* vp = static_cast<const char*>(a.v) + (size_t)u.k0 * a.v_token + (size_t)u.head * a.v_head;
+    const int r0 = wave * CHUNK_ROWS + lane / SLOTS;                       // row inside the tile, first chunk (the swizzle is the same for the others)
+    const int slot_off = ((lane % SLOTS) ^ swz<D>(r0)) * 16;
+    const int k_token = (int)a.k_token, v_token = (int)a.v_token;
+    auto issue = [&](int t, int buf) {
+        const int left = u.n_k - t * BKV;
+        const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)t * BKV * a.k_token), 0, (min(left, BKV) - 1) * k_token + ROWB, 0x00020000);
+        const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + (size_t)t * BKV * a.v_token), 0, (min(left, BKV) - 1) * v_token + ROWB, 0x00020000);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) {
+            const int row = min(r0 + c * 4 * CHUNK_ROWS, left - 1);
+            unsigned char* dst = smem[buf] + (wave + 4 * c) * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lptr_t)dst, 16, row * k_token + slot_off, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lptr_t)(dst + TILE_BYTES), 16, row * v_token + slot_off, 0, 0, 0);
+        }
+    };
+
+    const float c = PRE ? 1.f : a.scale * 1.4426950408889634f;
+    float m_run[2], l_run[2];
+    f32x4 o[DT][2];      // [16-feature tile][row tile]: features 16 dt + 4 q4 .. + 3 of row 16 qt + l16
+    auto clear = [&](float m) {
+        m_run[0] = m_run[1] = m;
+        l_run[0] = l_run[1] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++) o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+
+    const unsigned lds0 = (unsigned)(size_t)(lptr_t)&smem[0][0];
+    const unsigned kbase = lds0 + l16 * ROWB + ((kq ^ swz<D>(l16)) * 16);                    // + 64 ks by XOR, + 16 kt rows
+    const int v_key = 4 * q4 + l16 / 4;                                                     // transposing reads: 4 keys x 16 features per 16 lanes
+    const unsigned vbase = lds0 + TILE_BYTES + v_key * ROWB + (((l16 % 4) / 2) ^ swz<D>(v_key)) * 16 + (l16 % 2) * 8;   // + 32 dt by XOR, + 16 keys
+
+    auto tile = [&](int t, auto buf_tag, auto direct_tag) {
+        constexpr int BUF = decltype(buf_tag)::value;
+        constexpr bool DIRECT = decltype(direct_tag)::value;
+        constexpr int BUF_OFF = BUF * 2 * TILE_BYTES;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of tile t has landed
+        __builtin_amdgcn_s_barrier();                      // everyone's has; and the other buffer is free again
+        if (t + 1 < t_end) issue(t + 1, BUF ^ 1);
+        if (t * BKV > wave_max) return;                    // none of the wave's rows sees this tile
+        const bool masked = t * BKV + BKV - 1 > wave_min;
+
+        f32x4 s[4][2];   // [key tile][row tile]: keys 16 kt + 4 q4 .. + 3 of row 16 qt + l16
+#pragma unroll
+        for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++) s[kt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+            for (int kt = 0; kt < 4; kt++) {
+                const bf16x8 kf = *(const bf16x8 __attribute__((address_space(3)))*)((kbase ^ (ks * 64u)) + BUF_OFF + kt * 16 * ROWB);
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][ks], s[kt][qt], 0, 0, 0);
+            }
+        if (masked) {
+#pragma unroll
+            for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (t * BKV + kt * 16 + 4 * q4 + i > last[qt]) s[kt][qt][i] = -__builtin_inff();
+        }
+        __builtin_amdgcn_s_setprio(0);
+        bf16x8 pb[2][2];   // [32-key step][row tile]
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)__builtin_amdgcn_exp2f(PRE ? s[kt][qt][i] : s[kt][qt][i] * c);
+        } else {
+            float mx[2];
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++) {
+                float m0 = s[0][qt][0];
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++) m0 = max3(max3(s[kt][qt][0], s[kt][qt][1], m0), s[kt][qt][2], s[kt][qt][3]);
+                m0 = max3(m0, __shfl_xor(m0, 16, 64), m0);
+                mx[qt] = max3(m0, __shfl_xor(m0, 32, 64), m0);
+            }
+            const bool grow0 = (mx[0] - m_run[0]) * c > RESCALE_LOG2, grow1 = (mx[1] - m_run[1]) * c > RESCALE_LOG2;   // (only hidden keys so far: -inf - -inf, false)
+            if (__any(grow0 || grow1)) {
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++) {
+                    const bool grow = qt ? grow1 : grow0;
+                    const float m_new = grow ? mx[qt] : m_run[qt];
+                    const float corr = grow ? __builtin_amdgcn_exp2f((m_run[qt] - m_new) * c) : 1.f;
+                    m_run[qt] = m_new;
+                    l_run[qt] *= corr;
+#pragma unroll
+                    for (int dt = 0; dt < DT; dt++) o[dt][qt] *= corr;
+                }
+            }
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++) {
+                const float mc = m_run[qt] == -__builtin_inff() ? 0.f : m_run[qt] * c;
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[kt][qt][i], c, -mc));
+            }
+        }
+        __builtin_amdgcn_s_setprio(1);
+        const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+#pragma unroll
+        for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const bf16x2 pr = {pb[ks][qt][j], pb[ks][qt][j + 1]};
+                    l_run[qt] = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run[qt], false);
+                }
+
+        // O^T += V^T P^T
+        auto values = [&](auto clean_tag) {
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+                for (int ks = 0; ks < 2; ks++) {
+                    const unsigned at = (vbase ^ (dt * 32u)) + BUF_OFF + ks * 32 * ROWB;
+                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)at);
+                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(at + 16 * ROWB));
+                    bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    if constexpr (decltype(clean_tag)::value) {
+#pragma unroll
+                        for (int j = 0; j < 8; j++) vf[j] = not_finite(vf[j]) ? (bf16_t)0.f : vf[j];
+                    }
+#pragma unroll
+                    for (int qt = 0; qt < 2; qt++) o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[ks][qt], o[dt][qt], 0, 0, 0);
+                }
+        };
+        bool odd = false;        // infinities or NaN among the values of a tile that not all rows see
+        if (masked) {
+#pragma unroll 1
+            for (int j = lane; j < TILE_BYTES / 16; j += 64) {
+                const bf16x8 x = *(const bf16x8 __attribute__((address_space(3)))*)(lds0 + TILE_BYTES + BUF_OFF + j * 16);
+#pragma unroll
+                for (int e = 0; e < 8; e++) odd |= not_finite(x[e]);
+            }
+            odd = __any(odd);
+        }
+        if (odd) {
+            values(std::true_type{});
+#pragma unroll 1
+            for (int key = 0; key < BKV; key++) {
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) {
+                    const bf16x4 x = *(const bf16x4 __attribute__((address_space(3)))*)(lds0 + TILE_BYTES + BUF_OFF + key * ROWB + (((2 * dt + q4 / 2) ^ swz<D>(key)) * 16) + (q4 % 2) * 8);
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+#pragma unroll
+                        for (int qt = 0; qt < 2; qt++)
+                            if (not_finite(x[i]) && t * BKV + key <= last[qt]) o[dt][qt][i] += (float)x[i];
+                }
+            }
+        } else {
+            values(std::false_type{});
+        }
+    };
+    auto row_total = [&](float x) {
+        x += __shfl_xor(x, 16, 64);
+        return x + __shfl_xor(x, 32, 64);
+    };
+#define HYB_KEY_LOOP(direct_tag)                                                  \
+    if (t_begin < t_end) issue(t_begin, 0);                                       \
+    for (int t = t_begin; t < t_end; t += 2) {                                    \
+        tile(t, std::integral_constant<int, 0>{}, direct_tag);                    \
+        if (t + 1 < t_end) tile(t + 1, std::integral_constant<int, 1>{}, direct_tag); \
+    }
+    clear(0.f);
+    HYB_KEY_LOOP(std::true_type{})
+    {
+        bool out_of_range = false;
+#pragma unroll
+        for (int qt = 0; qt < 2; qt++) {
+            const float l = row_total(l_run[qt]);
+            // (a row that sees none of these keys has no sum to judge)
+            if (active && t_begin < t_end && last[qt] >= t_begin * BKV) out_of_range |= !(l > 0x1p-64f && l < 0x1p+64f);       // also true for NaN
+        }
+        const int wave_bad = __any(out_of_range) ? 1 : 0;
+        __syncthreads();                                     // every wave is done with the tile buffers
+        volatile int* flags = reinterpret_cast<volatile int*>(&smem[0][0]);
+        if (lane == 0) flags[wave] = wave_bad;
+        __syncthreads();
+        const bool again = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        __syncthreads();                                     // the flags are read before the buffers are refilled
+        if (again) {
+            clear(-__builtin_inff());
+            HYB_KEY_LOOP(std::false_type{})
+        }
+    }
+#undef HYB_KEY_LOOP
+
+#pragma unroll
+    for (int qt = 0; qt < 2; qt++) {
+        const float l = row_total(l_run[qt]);
+        if (wave * 32 + qt * 16 + l16 >= u.rows) continue;
+        const int row = u.row0 + wave * 32 + qt * 16 + l16;
+        const int tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+        if (a.parts > 1) {
+            const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
+            if (q4 == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
+            if (l != 0.f) {                                  // (nothing to merge otherwise)
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) *reinterpret_cast<f32x4*>(a.part + at * D + dt * 16 + 4 * q4) = o[dt][qt];
+            }
+            continue;
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;         // no key with a score above minus infinity: zeros
+        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 8 * q4;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+            *reinterpret_cast<bf16x4*>(op + dt * 32) = bf16x4{(bf16_t)(o[dt][qt][0] * inv), (bf16_t)(o[dt][qt][1] * inv), (bf16_t)(o[dt][qt][2] * inv), (bf16_t)(o[dt][qt][3] * inv)};
+    }
+}
+
+}  // namespace
+
+int hyb_launch_packed_attention_mfma(const PackedAttnArgs& a, int head_dim, hipStream_t st) {
+    const dim3 grid = packed_grid(a);
+    HybTraceScope trace("packed_attention_mfma", "byte", 4.0 * head_dim * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
+    if (head_dim == 64) {
+        if (a.prescaled) hipLaunchKernelGGL((packed_attention_kernel<64, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((packed_attention_kernel<64, false>), grid, dim3(256), 0, st, a);
+    } else {
+        if (a.prescaled) hipLaunchKernelGGL((packed_attention_kernel<128, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((packed_attention_kernel<128, false>), grid, dim3(256), 0, st, a);
+    }
+    return hyb_check_launch("packed_attention_mfma");
+}

@@ -1,0 +1,164 @@
+// Layout of a packed batch: offsets of the requests, and request index and (time, height, width) position of every token.
+//
+// Bound by what it writes, 16 bytes a row; small batches by launch latency.  Lengths are summed with an addition that
+// saturates at the capacity (associative, and exact for everything below it), so a prefix sum needs no 64-bit numbers.
+#include "common.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRowsPerThread = 4;       // 16 bytes of request indices and 48 bytes of positions: four full stores
+constexpr int kInOne = 2048;            // requests whose prefix sum every workgroup makes for itself (8 KB of LDS)
+
+__device__ __forceinline__ unsigned add_capped(unsigned a, unsigned b, unsigned cap) {   // a, b <= cap < 2^31
+    return min(a + b, cap);
+}
+
+__device__ __forceinline__ unsigned tokens_of(int4 s, unsigned cap) {
+    const unsigned long long f = max(s.x, 0), h = max(s.y, 0), w = max(s.z, 0), t = max(s.w, 0);
+    const unsigned long long fh = min(f * h, (unsigned long long)1 << 31);       // < 2^62 before, and the next product < 2^62 again
+    return (unsigned)min(fh * w + t, (unsigned long long)cap);
+}
+
+// Exclusive prefix sum of one value per thread; *total gets the sum.  wave_sums: LDS, kThreads / 64 values.
+__device__ __forceinline__ unsigned block_scan(unsigned x, unsigned cap, unsigned* wave_sums, unsigned* total) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    unsigned inc = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned below = __shfl_up(inc, o, 64);
+        if (lane >= o) inc = add_capped(inc, below, cap);
+    }
+    if (lane == 63) wave_sums[wave] = inc;
+    __syncthreads();
+    unsigned before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; w++) {
+        if (w < wave) before = add_capped(before, wave_sums[w], cap);
+        all = add_capped(all, wave_sums[w], cap);
+    }
+    __syncthreads();
+    *total = all;
+    unsigned excl = __shfl_up(inc, 1, 64);
+    if (lane == 0) excl = 0;
+    return add_capped(before, excl, cap);
+}
+
+// offsets[0 .. requests] by one workgroup, kThreads requests at a time.
+__global__ __launch_bounds__(kThreads) void packed_offsets_kernel(const int4* shapes, int requests, unsigned cap, int* offsets) {
+    __shared__ unsigned wave_sums[kThreads / 64];
+    unsigned carry = 0;
+    for (int s0 = 0; s0 < requests; s0 += kThreads) {
+        const int s = s0 + threadIdx.x;
+        unsigned all;
+        const unsigned before = block_scan(s < requests ? tokens_of(shapes[s], cap) : 0u, cap, wave_sums, &all);
+        if (s < requests) offsets[s] = (int)add_capped(carry, before, cap);
+        carry = add_capped(carry, all, cap);
+    }
+    if (threadIdx.x == 0) offsets[requests] = (int)carry;
+}
+
+struct Place { int request, t, y, x; };
+__device__ __forceinline__ Place place_of(int s, int4 sh, unsigned i, bool text_after) {
+    const unsigned f = max(sh.x, 0), h = max(sh.y, 0), w = max(sh.z, 0);
+    const unsigned long long hw = (unsigned long long)h * w;
+    // (an image of 2^32 tokens or more holds every row that fits; its row index still fits 32 bits)
+    const bool image = hw > 0xffffffffull ? f > 0 : (unsigned long long)f * hw > i;
+    if (image) {
+        const unsigned plane = hw > 0xffffffffull ? 0u : i / (unsigned)hw, in = hw > 0xffffffffull ? i : i - plane * (unsigned)hw;
+        return {s, (int)plane, (int)(in / w), (int)(in % w)};
+    }
+    const unsigned j = i - f * (unsigned)hw;
+    const int p = text_after ? (int)(max(f, max(h, w)) + j) : 0;
+    return {s, p, p, p};
+}
+
+// Four rows per thread.  SCAN: every workgroup sums the lengths in LDS itself (requests <= kInOne), the first writes the offsets too: one launch;
+// otherwise the offsets are there.
+template <bool SCAN>
+__global__ __launch_bounds__(kThreads) void packed_rows_kernel(const int4* shapes, int requests, unsigned cap, int text_after, int* offsets, int* request, int* positions) {
+    __shared__ unsigned own[SCAN ? kInOne + 1 : 1];
+    __shared__ unsigned wave_sums[kThreads / 64];
+    if constexpr (SCAN) {
+        unsigned carry = 0;
+        for (int s0 = 0; s0 < requests; s0 += kThreads) {
+            const int s = s0 + threadIdx.x;
+            unsigned all;
+            const unsigned before = block_scan(s < requests ? tokens_of(shapes[s], cap) : 0u, cap, wave_sums, &all);
+            if (s < requests) own[s] = add_capped(carry, before, cap);
+            carry = add_capped(carry, all, cap);
+        }
+        if (threadIdx.x == 0) own[requests] = carry;
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int s = threadIdx.x; s <= requests; s += kThreads) offsets[s] = (int)own[s];
+    }
+    auto first_row = [&](int s) { return SCAN ? own[s] : (unsigned)offsets[s]; };
+    const unsigned r0 = ((unsigned)blockIdx.x * kThreads + threadIdx.x) * kRowsPerThread, rows = first_row(requests);
+    if (r0 >= rows) return;
+    int s = 0;                                      // the last request that begins at or before r0 and is not empty: first_row(s) <= r0 < first_row(s + 1)
+    for (int len = requests; len > 1;) {
+        const int half = len / 2;
+        if (first_row(s + half) <= r0) { s += half; len -= half; }
+        else len = half;
+    }
+    int4 sh = shapes[s];
+    unsigned begin = first_row(s), end = first_row(s + 1);
+    const int count = (int)min(rows - r0, (unsigned)kRowsPerThread);
+    int req[kRowsPerThread], pos[kRowsPerThread][3];
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; i++) {
+        if (i >= count) { req[i] = pos[i][0] = pos[i][1] = pos[i][2] = 0; continue; }
+        while (r0 + i >= end) {                     // (ends: r0 + i < rows = the end of the last request)
+            s++;
+            begin = end;
+            end = first_row(s + 1);
+            sh = shapes[s];
+        }
+        const Place p = place_of(s, sh, r0 + i - begin, text_after != 0);
+        req[i] = p.request; pos[i][0] = p.t; pos[i][1] = p.y; pos[i][2] = p.x;
+    }
+    if (count == kRowsPerThread) {
+        if (request) *reinterpret_cast<int4*>(request + r0) = make_int4(req[0], req[1], req[2], req[3]);
+        if (positions) {
+            int4* dst = reinterpret_cast<int4*>(positions + (size_t)r0 * 3);
+            dst[0] = make_int4(pos[0][0], pos[0][1], pos[0][2], pos[1][0]);
+            dst[1] = make_int4(pos[1][1], pos[1][2], pos[2][0], pos[2][1]);
+            dst[2] = make_int4(pos[2][2], pos[3][0], pos[3][1], pos[3][2]);
+        }
+    } else {
+        for (int i = 0; i < count; i++) {
+            if (request) request[r0 + i] = req[i];
+            if (positions)
+                for (int a = 0; a < 3; a++) positions[(size_t)(r0 + i) * 3 + a] = pos[i][a];
+        }
+    }
+}
+
+}  // namespace
+
+extern "C" int hyb_packed_layout(const int* shapes, int requests, int capacity, int text_after, int* offsets, int* request, int* positions, void* stream) {
+    HYB_REQUIRE(requests >= 0 && capacity >= 0, HYB_ERR_SHAPE, "hyb_packed_layout: negative size");
+    HYB_CHECK_PTR(offsets); HYB_CHECK_ALIGN(offsets);
+    if (requests > 0) HYB_CHECK_PTR(shapes);
+    HYB_CHECK_ALIGN(shapes); HYB_CHECK_ALIGN(request); HYB_CHECK_ALIGN(positions);
+    const hipStream_t st = (hipStream_t)stream;
+    const int4* sh = reinterpret_cast<const int4*>(shapes);
+    const unsigned cap = (unsigned)capacity;
+    const bool rows = requests > 0 && capacity > 0 && (request || positions);
+    const int groups = (int)(((size_t)capacity + kThreads * kRowsPerThread - 1) / (kThreads * kRowsPerThread));
+    if (rows && requests <= kInOne) {
+        HybTraceScope trace("packed_layout", "byte", 16.0 * requests + 16.0 * capacity, st);
+        hipLaunchKernelGGL(packed_rows_kernel<true>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, offsets, request, positions);
+        return hyb_check_launch("packed_layout");
+    }
+    {
+        HybTraceScope trace("packed_offsets", "byte", 20.0 * requests, st);
+        hipLaunchKernelGGL(packed_offsets_kernel, dim3(1), dim3(kThreads), 0, st, sh, requests, cap, offsets);
+    }
+    const int rc = hyb_check_launch("packed_offsets");
+    if (rc != HYB_OK || !rows) return rc;
+    HybTraceScope trace("packed_layout", "byte", 16.0 * capacity, st);
+    hipLaunchKernelGGL(packed_rows_kernel<false>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, offsets, request, positions);
+    return hyb_check_launch("packed_layout");
+}
