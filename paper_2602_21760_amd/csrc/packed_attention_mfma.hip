@@ -14,7 +14,7 @@
 //
 // Masks: the last key that a row sees is one number per row (causal, or the end of the sequence); only tiles in which a wave's rows differ from
 // "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA, so such a tile is
-// searched for them first, and if there are any (never in sane data) they are zeroed in the fragments and added to the rows that see them.
+// searched for them first, and if there are any they are zeroed in the fragments and added to the rows that see them.
 #include "packed_attention.h"
 
 #include <type_traits>
@@ -41,60 +41,124 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 __device__ __forceinline__ bool not_finite(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
 
+// Transposing LDS reads of the V^T fragments of 32 output features (two 16-feature tiles, two 32-key steps of two reads each).  Written as asm so that they can be issued
+// ahead of their use: a wait that the compiler places before such a read through its builtin also waits for the next tile's copies.  Every result goes
+// through lds_wait(), which stands between these reads and their use and keeps the registers in use until they are written.
+template <int D>
+__device__ __forceinline__ void v_reads(unsigned at, bf16x4 (&vh)[2][2][2]) {
+    constexpr int ROWB = D * 2;
+#pragma unroll
+    for (int dd = 0; dd < 2; dd++)
+#pragma unroll
+        for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+            for (int half = 0; half < 2; half++)
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(vh[dd][ks][half]) : "v"(dd ? at ^ 32u : at), "i"((ks * 32 + half * 16) * ROWB));
+}
+// Waits until at most YOUNGER LDS reads are outstanding; reads complete in order.
+template <int YOUNGER>
+__device__ __forceinline__ void lds_wait(bf16x4 (&vh)[2][2][2], bf16x8 (&vf)[2][2]) {
+    asm volatile("s_waitcnt lgkmcnt(%8)"
+                 : "+v"(vh[0][0][0]), "+v"(vh[0][0][1]), "+v"(vh[0][1][0]), "+v"(vh[0][1][1]), "+v"(vh[1][0][0]), "+v"(vh[1][0][1]), "+v"(vh[1][1][0]), "+v"(vh[1][1][1])
+                 : "n"(YOUNGER));
+#pragma unroll
+    for (int dd = 0; dd < 2; dd++)
+#pragma unroll
+        for (int ks = 0; ks < 2; ks++) {
+            const bf16x4 lo = vh[dd][ks][0], hi = vh[dd][ks][1];
+            vf[dd][ks] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        }
+}
+
+// The same for a K fragment: requested, and awaited with at most YOUNGER reads outstanding.
+template <int OFFSET>
+__device__ __forceinline__ void k_read(unsigned at, bf16x8& f) { asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f) : "v"(at), "i"(OFFSET)); }
+template <int YOUNGER>
+__device__ __forceinline__ void k_wait(bf16x8& f) { asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(f) : "n"(YOUNGER)); }
+
+// f(0), f(1), ... f(N - 1) with the index as a type
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<N, I + 1>(f);
+    }
+}
+
+// The lane's index from an instruction the compiler cannot trace back: what rare paths and the epilogue derive from it is not kept in registers over the key loop.
+__device__ __forceinline__ int lane_again() {
+    int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 template <int D, bool PRE>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(PackedAttnArgs a) {
     constexpr int ROWB = D * 2, TILE_BYTES = BKV * ROWB, SLOTS = ROWB / 16;
     constexpr int CHUNK_ROWS = 1024 / ROWB, CHUNKS = BKV / CHUNK_ROWS / 4;      // rows of a 1 KB copy; copies per wave, operand and tile
-    constexpr int KS = D / 32, DT = D / 16;
+    constexpr int KS = D / 32, DT = D / 16, VG = D / 32;
+    constexpr unsigned OTHER = 2 * TILE_BYTES;                                  // XOR to the other buffer
     // [buffer][K tile | V tile]
-    __shared__ __attribute__((aligned(256))) unsigned char smem[2][2 * TILE_BYTES];
+    __shared__ __attribute__((aligned(4 * TILE_BYTES))) unsigned char smem[2][2 * TILE_BYTES];
+    __shared__ int row_last[BQ];         // last key that each row sees (read in masked tiles only)
 
     const PackedUnit u = packed_unit<BQ>(a);
     if (u.rows == 0) return;
-    const int tid = threadIdx.x, lane = tid % 64;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int lane = threadIdx.x % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int l16 = lane % 16, q4 = lane / 16;
     const int kq = (q4 >> 1) | ((q4 & 1) << 1);      // which 8 of a step's 32 features the lane holds (lanes i and i + 32 take neighbouring slots)
 
     // the lane's rows, one per 16-row tile (rows behind the block's last are copies of it, never stored)
-    int last[2];                                     // last key that the row sees
     bf16x8 qf[2][KS];
 #pragma unroll
     for (int qt = 0; qt < 2; qt++) {
         const int row = u.row0 + min(wave * 32 + qt * 16 + l16, u.rows - 1);
         const int t = row / a.group, g = row - t * a.group;
-        last[qt] = packed_last_key(a, u, t);
+        if (q4 == 0) row_last[wave * 32 + qt * 16 + l16] = packed_last_key(a, u, t);
         const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + g) * a.q_head;
 #pragma unroll
         for (int ks = 0; ks < KS; ks++) qf[qt][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 64 + kq * 16);
     }
     // the wave's rows see at least the keys 0 .. wave_min and at most 0 .. wave_max, the block's rows at most 0 .. block_max
-    const int wave_min = packed_last_key(a, u, (u.row0 + min(wave * 32, u.rows - 1)) / a.group);
     const bool active = wave * 32 < u.rows;
+    const int wave_min = packed_last_key(a, u, (u.row0 + min(wave * 32, u.rows - 1)) / a.group);
     const int wave_max = active ? packed_last_key(a, u, (u.row0 + min(wave * 32 + 31, u.rows - 1)) / a.group) : -1;
     const int block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
 
     const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;                    // (block_max == -1: no tile)
     const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
     const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
+    // Tiles t_begin .. plain_end - 1 are seen whole by all rows and followed by a tile of 64 keys: a loop of its own, which holds no masks in registers.
+    const int block_min = packed_last_key(a, u, u.row0 / a.group);
+    const int plain_end = min(min((block_min + 1) / BKV, u.n_k / BKV - 1), t_end - 1);
 
-    // Tile copy: lane i of a 1 KB chunk fills slot i % SLOTS of row i / SLOTS with feature vector slot ^ swz(row).  The tile's first row is in the
-    // resource (64-bit), so an offset never exceeds a tile.  Only the ragged last tile has its rows clamped.
+    // Tile copy: lane i of a 1 KB chunk fills slot i % SLOTS of row i / SLOTS with feature vector slot ^ swz(row) (the swizzle is the same for a wave's
+    // chunks).  The tile's first row is in the resource (64-bit), so an offset never exceeds a tile.  Only the ragged last tile has its rows clamped.
     const char* kp = static_cast<const char*>(a.k) + (size_t)u.k0 * a.k_token + (size_t)u.head * a.k_head;
     const char* vp = static_cast<const char*>(a.v) + (size_t)u.k0 * a.v_token + (size_t)u.head * a.v_head;
-    const int r0 = wave * CHUNK_ROWS + lane / SLOTS;                       // row inside the tile, first chunk (the swizzle is the same for the others)
-    const int slot_off = ((lane % SLOTS) ^ swz<D>(r0)) * 16;
     const int k_token = (int)a.k_token, v_token = (int)a.v_token;
-    auto issue = [&](int t, int buf) {
+    const int r0 = wave * CHUNK_ROWS + lane / SLOTS, slot_off = ((lane % SLOTS) ^ swz<D>(r0)) * 16;
+    const int k_off = r0 * k_token + slot_off, v_off = r0 * v_token + slot_off;
+    auto issue = [&](int t, int buf, auto whole_tag) {     // whole: the tile has 64 keys
         const int left = u.n_k - t * BKV;
         const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)t * BKV * a.k_token), 0, (min(left, BKV) - 1) * k_token + ROWB, 0x00020000);
         const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + (size_t)t * BKV * a.v_token), 0, (min(left, BKV) - 1) * v_token + ROWB, 0x00020000);
+        unsigned char* dst = smem[buf] + wave * 1024;
+        if (decltype(whole_tag)::value || left >= BKV) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; c++) {
-            const int row = min(r0 + c * 4 * CHUNK_ROWS, left - 1);
-            unsigned char* dst = smem[buf] + (wave + 4 * c) * 1024;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lptr_t)dst, 16, row * k_token + slot_off, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lptr_t)(dst + TILE_BYTES), 16, row * v_token + slot_off, 0, 0, 0);
+            for (int c = 0; c < CHUNKS; c++) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lptr_t)(dst + c * 4096), 16, k_off, c * 4 * CHUNK_ROWS * k_token, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lptr_t)(dst + c * 4096 + TILE_BYTES), 16, v_off, c * 4 * CHUNK_ROWS * v_token, 0, 0);
+            }
+        } else {
+            const int ln = lane_again(), first = wave * CHUNK_ROWS + ln / SLOTS, so = ((ln % SLOTS) ^ swz<D>(first)) * 16;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; c++) {
+                const int row = min(first + c * 4 * CHUNK_ROWS, left - 1);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lptr_t)(dst + c * 4096), 16, row * k_token + so, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lptr_t)(dst + c * 4096 + TILE_BYTES), 16, row * v_token + so, 0, 0, 0);
+            }
         }
     };
 
@@ -110,45 +174,71 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             for (int qt = 0; qt < 2; qt++) o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
 
+    // LDS addresses of the fragments, one for K and one for V^T, in the buffer of the current tile; everything else is a constant XOR or offset
     const unsigned lds0 = (unsigned)(size_t)(lptr_t)&smem[0][0];
-    const unsigned kbase = lds0 + l16 * ROWB + ((kq ^ swz<D>(l16)) * 16);                    // + 64 ks by XOR, + 16 kt rows
     const int v_key = 4 * q4 + l16 / 4;                                                     // transposing reads: 4 keys x 16 features per 16 lanes
-    const unsigned vbase = lds0 + TILE_BYTES + v_key * ROWB + (((l16 % 4) / 2) ^ swz<D>(v_key)) * 16 + (l16 % 2) * 8;   // + 32 dt by XOR, + 16 keys
+    unsigned kb = lds0 + l16 * ROWB + ((kq ^ swz<D>(l16)) * 16);                            // + 64 ks by XOR, + 16 kt rows
+    unsigned vb = lds0 + TILE_BYTES + v_key * ROWB + (((l16 % 4) / 2) ^ swz<D>(v_key)) * 16 + (l16 % 2) * 8;   // + 32 dt by XOR, + 16 keys
 
-    auto tile = [&](int t, auto buf_tag, auto direct_tag) {
-        constexpr int BUF = decltype(buf_tag)::value;
-        constexpr bool DIRECT = decltype(direct_tag)::value;
-        constexpr int BUF_OFF = BUF * 2 * TILE_BYTES;
+    // PLAIN: all of the block's rows see all of the tile, and the next tile is whole
+    auto tile = [&](int t, int buf, auto direct_tag, auto plain_tag) {
+        constexpr bool DIRECT = decltype(direct_tag)::value, PLAIN = decltype(plain_tag)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of tile t has landed
         __builtin_amdgcn_s_barrier();                      // everyone's has; and the other buffer is free again
-        if (t + 1 < t_end) issue(t + 1, BUF ^ 1);
-        if (t * BKV > wave_max) return;                    // none of the wave's rows sees this tile
-        const bool masked = t * BKV + BKV - 1 > wave_min;
+        if (PLAIN || t + 1 < t_end) issue(t + 1, buf ^ 1, plain_tag);
+        if (PLAIN ? !active : t * BKV > wave_max) return;  // none of the wave's rows sees this tile
+        const bool masked = !PLAIN && t * BKV + BKV - 1 > wave_min;
 
+        // S^T = K Q^T; the K fragments (step j / 4, key tile j % 4) flow through a ring of four reads that run ahead of the MFMAs
+        bf16x8 ring[4];
+        __builtin_amdgcn_s_setprio(1);
+        auto k_frag = [&](auto j) { k_read<(j.value & 3) * 16 * ROWB>(kb ^ ((j.value >> 2) * 64u), ring[j.value & 3]); };
+        unrolled<4>(k_frag);
         f32x4 s[4][2];   // [key tile][row tile]: keys 16 kt + 4 q4 .. + 3 of row 16 qt + l16
 #pragma unroll
         for (int kt = 0; kt < 4; kt++)
 #pragma unroll
             for (int qt = 0; qt < 2; qt++) s[kt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        __builtin_amdgcn_s_setprio(1);
+        unrolled<4 * KS>([&](auto j) {
+            constexpr int J = j.value;
+            k_wait<(4 * KS - 1 - J < 3 ? 4 * KS - 1 - J : 3)>(ring[J & 3]);
 #pragma unroll
-        for (int ks = 0; ks < KS; ks++)
-#pragma unroll
-            for (int kt = 0; kt < 4; kt++) {
-                const bf16x8 kf = *(const bf16x8 __attribute__((address_space(3)))*)((kbase ^ (ks * 64u)) + BUF_OFF + kt * 16 * ROWB);
-#pragma unroll
-                for (int qt = 0; qt < 2; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][ks], s[kt][qt], 0, 0, 0);
-            }
+            for (int qt = 0; qt < 2; qt++) s[J & 3][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[J & 3], qf[qt][J >> 2], s[J & 3][qt], 0, 0, 0);
+            if constexpr (J + 4 < 4 * KS) k_frag(std::integral_constant<int, J + 4>{});
+        });
+
+        bf16x4 vh[2][2][2][2];   // [two groups of 32 features in flight][16-feature tile][32-key step][read]
+        bool odd = false;        // infinities or NaN among the values of a tile that not all rows see
         if (masked) {
+            const int ln = lane_again();
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++) {
+                const int seen = row_last[wave * 32 + qt * 16 + ln % 16] - t * BKV - 4 * (ln / 16);     // keys 16 kt + i > seen are hidden
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (kt * 16 + i > seen) s[kt][qt][i] = -__builtin_inff();
+            }
+            unsigned any = 0;
+#pragma unroll 1
+            for (int j = 0; j < TILE_BYTES / 1024; j++) {
+                const u32x4 x = *(const u32x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + j * 1024 + ln * 16);
+#pragma unroll
+                for (int e = 0; e < 4; e++) any |= ((x[e] & 0x7f80u) == 0x7f80u) | ((x[e] & 0x7f800000u) == 0x7f800000u);
+            }
+            odd = __any(any != 0);
+        }
+        if constexpr (DIRECT) v_reads<D>(vb, vh[0]);       // (the form with row maxima holds more values meanwhile and requests them after them)
+        // the exponentiated scores of key tiles 2 ks, 2 ks + 1, rounded to bf16, are the B operand of 32-key step ks
+        if constexpr (DIRECT && !PRE) {
 #pragma unroll
             for (int kt = 0; kt < 4; kt++)
 #pragma unroll
-                for (int qt = 0; qt < 2; qt++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (t * BKV + kt * 16 + 4 * q4 + i > last[qt]) s[kt][qt][i] = -__builtin_inff();
+                for (int qt = 0; qt < 2; qt++) s[kt][qt] *= c;
+            asm volatile("" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]), "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
         }
-        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_s_setprio(0);     // a wave yields during its exponentials, so that they do not hold up another wave's MFMAs
         bf16x8 pb[2][2];   // [32-key step][row tile]
         if constexpr (DIRECT) {
 #pragma unroll
@@ -156,8 +246,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
 #pragma unroll
                 for (int qt = 0; qt < 2; qt++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)__builtin_amdgcn_exp2f(PRE ? s[kt][qt][i] : s[kt][qt][i] * c);
+                    for (int i = 0; i < 4; i++) s[kt][qt][i] = __builtin_amdgcn_exp2f(s[kt][qt][i]);
+            asm volatile("" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]), "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)s[kt][qt][i];
         } else {
             float mx[2];
 #pragma unroll
@@ -189,84 +286,101 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
 #pragma unroll
                     for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[kt][qt][i], c, -mc));
             }
+            asm volatile("" : "+v"(pb[0][0]), "+v"(pb[0][1]), "+v"(pb[1][0]), "+v"(pb[1][1]));
+            __builtin_amdgcn_s_setprio(1);
+            v_reads<D>(vb, vh[0]);
         }
-        __builtin_amdgcn_s_setprio(1);
-        const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-#pragma unroll
-        for (int ks = 0; ks < 2; ks++)
-#pragma unroll
-            for (int qt = 0; qt < 2; qt++)
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const bf16x2 pr = {pb[ks][qt][j], pb[ks][qt][j + 1]};
-                    l_run[qt] = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run[qt], false);
-                }
 
-        // O^T += V^T P^T
-        auto values = [&](auto clean_tag) {
+        // O^T += V^T P^T, 32 features at a time, the next 32 on their way
 #pragma unroll
-            for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-                for (int ks = 0; ks < 2; ks++) {
-                    const unsigned at = (vbase ^ (dt * 32u)) + BUF_OFF + ks * 32 * ROWB;
-                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)at);
-                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(at + 16 * ROWB));
-                    bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    if constexpr (decltype(clean_tag)::value) {
-#pragma unroll
-                        for (int j = 0; j < 8; j++) vf[j] = not_finite(vf[j]) ? (bf16_t)0.f : vf[j];
-                    }
-#pragma unroll
-                    for (int qt = 0; qt < 2; qt++) o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[ks][qt], o[dt][qt], 0, 0, 0);
-                }
-        };
-        bool odd = false;        // infinities or NaN among the values of a tile that not all rows see
-        if (masked) {
-#pragma unroll 1
-            for (int j = lane; j < TILE_BYTES / 16; j += 64) {
-                const bf16x8 x = *(const bf16x8 __attribute__((address_space(3)))*)(lds0 + TILE_BYTES + BUF_OFF + j * 16);
-#pragma unroll
-                for (int e = 0; e < 8; e++) odd |= not_finite(x[e]);
+        for (int g = 0; g < VG; g++) {
+            bf16x8 vf[2][2];
+            if (g + 1 < VG) {
+                v_reads<D>(vb ^ ((g + 1) * 64u), vh[(g + 1) & 1]);
+                lds_wait<8>(vh[g & 1], vf);
+            } else {
+                lds_wait<0>(vh[g & 1], vf);
             }
-            odd = __any(odd);
+            if (odd) {
+#pragma unroll
+                for (int dd = 0; dd < 2; dd++)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+                        for (int j = 0; j < 8; j++) vf[dd][ks][j] = not_finite(vf[dd][ks][j]) ? (bf16_t)0.f : vf[dd][ks][j];
+            }
+#pragma unroll
+            for (int dd = 0; dd < 2; dd++)
+#pragma unroll
+                for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+                    for (int qt = 0; qt < 2; qt++) o[2 * g + dd][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dd][ks], pb[ks][qt], o[2 * g + dd][qt], 0, 0, 0);
+            if (g == 0) {        // the normaliser, from the rounded probabilities, beside the MFMAs
+                const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+#pragma unroll
+                for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+                    for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2) {
+                            const bf16x2 pr = {pb[ks][qt][j], pb[ks][qt][j + 1]};
+                            l_run[qt] = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run[qt], false);
+                        }
+            }
         }
         if (odd) {
-            values(std::true_type{});
+            const int ln = lane_again();
 #pragma unroll 1
             for (int key = 0; key < BKV; key++) {
+                bool seen[2];
+#pragma unroll
+                for (int qt = 0; qt < 2; qt++) seen[qt] = t * BKV + key <= row_last[wave * 32 + qt * 16 + ln % 16];
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) {
-                    const bf16x4 x = *(const bf16x4 __attribute__((address_space(3)))*)(lds0 + TILE_BYTES + BUF_OFF + key * ROWB + (((2 * dt + q4 / 2) ^ swz<D>(key)) * 16) + (q4 % 2) * 8);
+                    const bf16x4 x = *(const bf16x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + key * ROWB + (((2 * dt + ln / 32) ^ swz<D>(key)) * 16) + (ln / 16 % 2) * 8);
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
+                    for (int i = 0; i < 4; i++) {
+                        const float add = not_finite(x[i]) ? (float)x[i] : 0.f;
 #pragma unroll
-                        for (int qt = 0; qt < 2; qt++)
-                            if (not_finite(x[i]) && t * BKV + key <= last[qt]) o[dt][qt][i] += (float)x[i];
+                        for (int qt = 0; qt < 2; qt++) o[dt][qt][i] += seen[qt] ? add : 0.f;
+                    }
                 }
             }
-        } else {
-            values(std::false_type{});
         }
     };
     auto row_total = [&](float x) {
         x += __shfl_xor(x, 16, 64);
         return x + __shfl_xor(x, 32, 64);
     };
-#define HYB_KEY_LOOP(direct_tag)                                                  \
-    if (t_begin < t_end) issue(t_begin, 0);                                       \
-    for (int t = t_begin; t < t_end; t += 2) {                                    \
-        tile(t, std::integral_constant<int, 0>{}, direct_tag);                    \
-        if (t + 1 < t_end) tile(t + 1, std::integral_constant<int, 1>{}, direct_tag); \
-    }
+    auto key_loop = [&](auto direct_tag) {
+        if (t_begin < t_end) issue(t_begin, 0, std::false_type{});
+        int t = t_begin, buf = 0;
+        if constexpr (decltype(direct_tag)::value) {
+            for (; t < plain_end; t++, buf ^= 1) {
+                tile(t, buf, direct_tag, std::true_type{});
+                kb ^= OTHER;
+                vb ^= OTHER;
+            }
+        }
+        for (; t < t_end; t++, buf ^= 1) {
+            tile(t, buf, direct_tag, std::false_type{});
+            kb ^= OTHER;
+            vb ^= OTHER;
+        }
+        if ((t_end - t_begin) & 1) {     // back to the first buffer
+            kb ^= OTHER;
+            vb ^= OTHER;
+        }
+    };
     clear(0.f);
-    HYB_KEY_LOOP(std::true_type{})
+    key_loop(std::true_type{});
     {
         bool out_of_range = false;
 #pragma unroll
         for (int qt = 0; qt < 2; qt++) {
             const float l = row_total(l_run[qt]);
             // (a row that sees none of these keys has no sum to judge)
-            if (active && t_begin < t_end && last[qt] >= t_begin * BKV) out_of_range |= !(l > 0x1p-64f && l < 0x1p+64f);       // also true for NaN
+            if (active && t_begin < t_end && row_last[wave * 32 + qt * 16 + lane_again() % 16] >= t_begin * BKV) out_of_range |= !(l > 0x1p-64f && l < 0x1p+64f);       // also true for NaN
         }
         const int wave_bad = __any(out_of_range) ? 1 : 0;
         __syncthreads();                                     // every wave is done with the tile buffers
@@ -277,28 +391,28 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
         __syncthreads();                                     // the flags are read before the buffers are refilled
         if (again) {
             clear(-__builtin_inff());
-            HYB_KEY_LOOP(std::false_type{})
+            key_loop(std::false_type{});
         }
     }
-#undef HYB_KEY_LOOP
 
+    const int le = lane_again(), l16e = le % 16, q4e = le / 16;
 #pragma unroll
     for (int qt = 0; qt < 2; qt++) {
         const float l = row_total(l_run[qt]);
-        if (wave * 32 + qt * 16 + l16 >= u.rows) continue;
-        const int row = u.row0 + wave * 32 + qt * 16 + l16;
+        if (wave * 32 + qt * 16 + l16e >= u.rows) continue;
+        const int row = u.row0 + wave * 32 + qt * 16 + l16e;
         const int tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
         if (a.parts > 1) {
             const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
-            if (q4 == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
+            if (q4e == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
             if (l != 0.f) {                                  // (nothing to merge otherwise)
 #pragma unroll
-                for (int dt = 0; dt < DT; dt++) *reinterpret_cast<f32x4*>(a.part + at * D + dt * 16 + 4 * q4) = o[dt][qt];
+                for (int dt = 0; dt < DT; dt++) *reinterpret_cast<f32x4*>(a.part + at * D + dt * 16 + 4 * q4e) = o[dt][qt];
             }
             continue;
         }
         const float inv = l == 0.f ? 0.f : 1.0f / l;         // no key with a score above minus infinity: zeros
-        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 8 * q4;
+        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 8 * q4e;
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
             *reinterpret_cast<bf16x4*>(op + dt * 32) = bf16x4{(bf16_t)(o[dt][qt][0] * inv), (bf16_t)(o[dt][qt][1] * inv), (bf16_t)(o[dt][qt][2] * inv), (bf16_t)(o[dt][qt][3] * inv)};
