@@ -17,46 +17,58 @@ struct PackedAttnArgs {
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
     int blocks;                                   // row blocks of all sequences, an upper bound (see find_block)
     int parts, part_keys;                         // keys are cut into `parts` of part_keys keys (the last part takes what is left); 1: not cut
-    float* part;                                  // parts > 1: PartRows
+                                                  // (few-rows kernel: 1, and pieces of part_keys keys)
+    int pieces;                                   // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
+    float* part;                                  // scratch (see below)
     int xcd_heads, xcd_share;                     // gcd(8, k_heads), 8 / gcd
 };
 
-// Scratch of cut keys: for each (row of q, head) `parts` unnormalised accumulators of head_dim values, then for each `parts` pairs (reference, sum).
+// Scratch of cut keys.  Blocks of rows that are cut (all but the few-rows kernel): for each (row of q, head) `parts` unnormalised accumulators of head_dim values, then for each `parts` pairs (reference, sum).
 __host__ __device__ inline size_t packed_part_floats(int total_q, int q_heads, int parts, int head_dim) {
     return (size_t)total_q * q_heads * parts * (head_dim + 2);
 }
 
+// The few-rows kernel numbers pieces of part_keys keys: for each (piece, key head) 16 rows of head_dim values, then for each 16 pairs.
+__host__ __device__ inline size_t packed_piece_rows(int pieces, int k_heads) { return (size_t)pieces * k_heads * 16; }
+
 int hyb_launch_packed_attention_mfma(const PackedAttnArgs& a, int head_dim, hipStream_t st);
+int hyb_launch_packed_attention_few(const PackedAttnArgs& a, int head_dim, hipStream_t st);
 int hyb_launch_packed_attention_f32(const PackedAttnArgs& a, int head_dim, hipStream_t st);
 
 constexpr int kPackedRowsMfma = 128;                                                 // rows of a block: bf16
+constexpr int kPackedRowsFew = 16;                                                   // bf16, few rows per sequence
+constexpr int kPackedRowsMerge = 4;                                                  // merge of cut keys: a wave per row
+constexpr int kPackedMaxParts = 64;                                                  // its lanes hold a part's weight each
 constexpr int packed_rows_f32(int head_dim) { return head_dim == 64 ? 32 : 16; }     // fp32
 
 // Most blocks of `rows` rows that any offsets can ask for.
 inline long long packed_blocks(const PackedAttnArgs& a, int rows) { return (long long)a.total_q * a.group / rows + a.sequences; }
 
 // Workgroups of a launch.  A grid dimension holds less than 2^32 threads: what goes beyond 2^23 workgroups goes into the second one.
-inline dim3 packed_grid(const PackedAttnArgs& a) {
-    const size_t per_head = (size_t)((a.blocks + a.xcd_share - 1) / a.xcd_share) * a.parts;
-    const size_t total = 8 * (size_t)(a.k_heads / a.xcd_heads) * per_head, x = total < ((size_t)1 << 23) ? total : (size_t)1 << 23;
+inline dim3 packed_grid_of(size_t total) {
+    const size_t x = total < ((size_t)1 << 23) ? total : (size_t)1 << 23;
     return dim3((unsigned)x, (unsigned)((total + x - 1) / x));
+}
+inline dim3 packed_grid(const PackedAttnArgs& a) {
+    return packed_grid_of(8 * (size_t)(a.k_heads / a.xcd_heads) * ((a.blocks + a.xcd_share - 1) / a.xcd_share) * a.parts);
 }
 
 // Rows of a sequence after the offsets are brought into 0 .. total.
 __device__ __forceinline__ int packed_offset(const int* offsets, int s, int total) { return min(max(offsets[s], 0), total); }
 
-// Blocks are numbered without a table: sequence s begins at block floor(first row / ROWS) + s, which leaves every sequence at least as
-// many numbers as it has blocks of ROWS rows (floor(x + n) - floor(x) + 1 >= ceil(n)); the numbers left over have no rows.  The sequence of a
-// number is the last one that begins at or before it, found by all lanes of the wave at once, 64 candidates a step.
-template <int ROWS>
-__device__ __forceinline__ int packed_sequence_of(const PackedAttnArgs& a, int block) {
+// Pieces of sequences are numbered without a table: with `per` pieces' worth of rows (a block of query rows, a part of the keys) sequence s begins at number
+// floor(first row / per) + s, which leaves every sequence at least as many numbers as it has pieces, and at least one (floor(x + n) - floor(x) + 1 >=
+// ceil(n)); numbers left over have no rows.  The sequence of a number is the last one that begins at or before it, found by all lanes of the wave at
+// once, 64 candidates a step.
+__device__ __forceinline__ int packed_first_piece(const int* offsets, int s, int total, int mul, int per) {
+    return (int)((long long)packed_offset(offsets, s, total) * mul / per) + s;
+}
+__device__ __forceinline__ int packed_sequence_of(const int* offsets, int sequences, int total, int mul, int per, int piece) {
     const int lane = threadIdx.x % 64;
-    int lo = 0, len = a.sequences;
+    int lo = 0, len = sequences;
     while (len > 1) {
-        const int step = (len + 63) / 64, s = lo + lane * step;
-        const bool begins = lane * step < len &&
-                            (int)((long long)packed_offset(a.offsets_q, min(s, a.sequences - 1), a.total_q) * a.group / ROWS) + s <= block;
-        const int count = __popcll(__ballot(begins));
+        const int step = (len + 63) / 64, s = min(lo + lane * step, sequences - 1);
+        const int count = __popcll(__ballot(lane * step < len && packed_first_piece(offsets, s, total, mul, per) <= piece));
         const int at = count > 0 ? count - 1 : 0;
         lo += at * step;
         len = min(step, len - at * step);
@@ -70,7 +82,14 @@ struct PackedUnit {
     int row0, rows;              // first row of the block in its sequence, rows of the block (<= ROWS)
     int q0, k0;                  // first row of the sequence in q / o and in k / v
     int n_q, n_k;
+    int sequence;
 };
+__device__ __forceinline__ void packed_rows_of(const PackedAttnArgs& a, int s, PackedUnit& u) {
+    u.q0 = packed_offset(a.offsets_q, s, a.total_q);
+    u.k0 = packed_offset(a.offsets_k, s, a.total_k);
+    u.n_q = packed_offset(a.offsets_q, s + 1, a.total_q) - u.q0;
+    u.n_k = max(packed_offset(a.offsets_k, s + 1, a.total_k) - u.k0, 0);
+}
 template <int ROWS>
 __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
     PackedUnit u = {};
@@ -86,14 +105,12 @@ __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
     u.part = (int)(j % (unsigned)a.parts);
     const int block = a.blocks - 1 - ((int)(j / (unsigned)a.parts) * a.xcd_share + sx);
     if (block < 0) return u;
-    const int s = packed_sequence_of<ROWS>(a, block);
-    const int q0 = packed_offset(a.offsets_q, s, a.total_q), k0 = packed_offset(a.offsets_k, s, a.total_k);
-    const long long first = (long long)q0 * a.group / ROWS + s;
+    const int s = packed_sequence_of(a.offsets_q, a.sequences, a.total_q, a.group, ROWS, block);
+    const int first = packed_first_piece(a.offsets_q, s, a.total_q, a.group, ROWS);
     if (first > block) return u;
-    u.q0 = q0; u.k0 = k0;
-    u.n_q = packed_offset(a.offsets_q, s + 1, a.total_q) - q0;
-    u.n_k = max(packed_offset(a.offsets_k, s + 1, a.total_k) - k0, 0);
-    const long long all = (long long)max(u.n_q, 0) * a.group, row0 = (block - first) * ROWS;
+    packed_rows_of(a, s, u);
+    u.sequence = s;
+    const long long all = (long long)max(u.n_q, 0) * a.group, row0 = (long long)(block - first) * ROWS;
     u.rows = (int)max(min(all - row0, (long long)ROWS), 0ll);
     u.row0 = (int)row0;           // (meaningful when rows > 0: below total_q * group, which the launcher keeps below 2^31)
     return u;
@@ -102,4 +119,26 @@ __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
 // Last key that query t of a sequence sees (-1: none).
 __device__ __forceinline__ int packed_last_key(const PackedAttnArgs& a, const PackedUnit& u, int t) {
     return a.causal ? max(min(t + u.n_k - u.n_q, u.n_k - 1), -1) : u.n_k - 1;
+}
+
+// Infinities and NaN (exponent bits all ones), found and blanked without comparisons, which would need a scalar register pair per value: the exponent field
+// plus its lowest bit carries into the sign's place.  bf16: two values per word.
+__device__ __forceinline__ unsigned odd_bits_bf16(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ unsigned odd_mask_bf16(unsigned x) {    // all ones in the places of such values
+    const unsigned h = odd_bits_bf16(x);
+    return (h << 1) - (h >> 15);
+}
+__device__ __forceinline__ unsigned odd_bits_f32(unsigned x) { return ((x & 0x7f800000u) + 0x00800000u) & 0x80000000u; }
+__device__ __forceinline__ unsigned odd_mask_f32(unsigned x) { return (unsigned)((int)odd_bits_f32(x) >> 31); }
+
+__device__ __forceinline__ void keep_finite(bf16x4& x) {
+    u32x2 w = __builtin_bit_cast(u32x2, x);
+    w[0] &= ~odd_mask_bf16(w[0]);
+    w[1] &= ~odd_mask_bf16(w[1]);
+    x = __builtin_bit_cast(bf16x4, w);
+}
+// The infinities and NaN among four values where `seen` (0 or all ones) says so, zeros elsewhere.
+__device__ __forceinline__ f32x4 only_odd(u32x2 w, unsigned seen) {
+    const unsigned a = w[0] & odd_mask_bf16(w[0]) & seen, b = w[1] & odd_mask_bf16(w[1]) & seen;
+    return f32x4{__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
 }

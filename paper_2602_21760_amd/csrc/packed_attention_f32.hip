@@ -19,8 +19,6 @@ __device__ __forceinline__ float exp_neg(float x) {
     return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
 }
 
-__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
-
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
     constexpr int BQ = packed_rows_f32(D), QT = BQ / 16, DT = D / 16, VH = D / 64;
@@ -115,8 +113,8 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
                 }
         }
         // a probability of 0 does not keep an infinity or NaN of a hidden key's value out of the MFMA: such values are added to the rows that see them by hand
-        bool odd = false;
         if (masked) {
+            unsigned any = 0;
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
@@ -124,30 +122,29 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 #pragma unroll
                     for (int h = 0; h < VH; h++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) odd |= not_finite(v[kt][i][h][e]);
-            odd = __any(odd);
-        }
-        if (odd) {
+                        for (int e = 0; e < 4; e++) any |= odd_bits_f32(__float_as_uint(v[kt][i][h][e]));
+            if (__any(any != 0)) {
 #pragma unroll 1
-            for (int key = key0; key < min(key0 + BKV, u.n_k); key++) {
+                for (int key = key0; key < min(key0 + BKV, u.n_k); key++) {
 #pragma unroll
-                for (int dt = 0; dt < DT; dt++)
+                    for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float x = *reinterpret_cast<const float*>(vp + (size_t)key * a.v_token + 4 * ((dt / 4) * 64 + 16 * q4 + 4 * i + dt % 4));
+                        for (int i = 0; i < 4; i++) {
+                            unsigned x = *reinterpret_cast<const unsigned*>(vp + (size_t)key * a.v_token + 4 * ((dt / 4) * 64 + 16 * q4 + 4 * i + dt % 4));
+                            x &= odd_mask_f32(x);
 #pragma unroll
-                        for (int qt = 0; qt < QT; qt++)
-                            if (not_finite(x) && key <= last[qt]) o[dt][qt][i] += x;
-                    }
+                            for (int qt = 0; qt < QT; qt++) o[dt][qt][i] += __uint_as_float(x & (key <= last[qt] ? ~0u : 0u));
+                        }
+                }
+#pragma unroll
+                for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+#pragma unroll
+                        for (int h = 0; h < VH; h++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) v[kt][i][h][e] = __uint_as_float(__float_as_uint(v[kt][i][h][e]) & ~odd_mask_f32(__float_as_uint(v[kt][i][h][e])));
             }
-#pragma unroll
-            for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-#pragma unroll
-                    for (int h = 0; h < VH; h++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) v[kt][i][h][e] = not_finite(v[kt][i][h][e]) ? 0.f : v[kt][i][h][e];
         }
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
@@ -211,63 +208,77 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 }
 
 // Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
-// (fp32: e^(m_p - M)), M = max m_p over the parts with keys, parts in index order.  One thread per 4 features.  Bound by the partial results it reads.
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, float c) {
-    const int parts = a.parts;
-    a.parts = 1;                          // a workgroup per (block, head)
-    const PackedUnit u = packed_unit<ROWS>(a);
-    const float* ml0 = a.part + (size_t)a.total_q * a.q_heads * parts * D;
-    for (int i = threadIdx.x; i < u.rows * (D / 4); i += 256) {
-        const int row = u.row0 + i / (D / 4), f = i % (D / 4) * 4;
-        const int tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
-        const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * parts;
-        const f32x2* ml = reinterpret_cast<const f32x2*>(ml0) + at;
-        float m_all = -__builtin_inff();
-        for (int p = 0; p < parts; p++)
-            if (ml[p][1] != 0.f) m_all = fmaxf(m_all, ml[p][0]);
-        float l = 0.f;
-        f32x4 r = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < parts; p++) {
-            if (ml[p][1] == 0.f) continue;
-            const float d = ml[p][0] - m_all;
-            const float w = ml[p][0] == m_all ? 1.f : sizeof(T) == 4 ? exp_neg(d) : __builtin_amdgcn_exp2f(d * c);
-            l = fmaf(ml[p][1], w, l);
-            const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + (at + p) * D + f);
+// (fp32: e^(m_p - M)), M = max m_p over the parts with keys, parts in index order.  A wave per row: lane p has the weight of part p, every lane D / 64 features.
+// Bound by the latency of two loads and, for many rows, by the partial results it reads.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, int parts, float c) {
+    constexpr int N = D / 64;
+    const PackedUnit u = packed_unit<kPackedRowsMerge>(a);
+    const int lane = threadIdx.x % 64, r = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (r >= u.rows) return;
+    const int row = u.row0 + r, tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+    const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * parts;
+    const float* o = a.part + at * D + lane * N;
+    f32x2 ml = {-__builtin_inff(), 0.f};
+    if (lane < parts) ml = *reinterpret_cast<const f32x2*>(a.part + (size_t)a.total_q * a.q_heads * parts * D + (at + lane) * 2);
+    const bool any = ml[1] != 0.f;       // (a part without keys for this row: its accumulators were not written)
+    const float m_all = wave_max(any ? ml[0] : -__builtin_inff()), d = ml[0] - m_all;
+    const float w = !any ? 0.f : ml[0] == m_all ? 1.f : sizeof(T) == 4 ? exp_neg(d) : __builtin_amdgcn_exp2f(d * c);
+    float l = any ? ml[1] * w : 0.f, x[N];
+    l = wave_sum(l);
 #pragma unroll
-            for (int e = 0; e < 4; e++) r[e] = fmaf(v[e], w, r[e]);
-        }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        T* op = reinterpret_cast<T*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head) + f;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(op) = r * inv;
-        else *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16_t)(r[0] * inv), (bf16_t)(r[1] * inv), (bf16_t)(r[2] * inv), (bf16_t)(r[3] * inv)};
+    for (int e = 0; e < N; e++) x[e] = 0.f;
+    const unsigned long long with_keys = __ballot(any);
+#pragma unroll 8
+    for (int p = 0; p < parts; p++) {
+        const float wp = __shfl(w, p, 64);
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = o[(size_t)p * D + e];
+#pragma unroll
+        for (int e = 0; e < N; e++) x[e] = with_keys >> p & 1 ? fmaf(v[e], wp, x[e]) : x[e];
     }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    T* op = reinterpret_cast<T*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head) + lane * N;
+#pragma unroll
+    for (int e = 0; e < N; e++) op[e] = from_f32<T>(x[e] * inv);
 }
 
-template <typename T, int D, int ROWS>
-int launch_merge(PackedAttnArgs a, hipStream_t st) {
-    const float c = a.prescaled ? 1.f : a.scale * 1.4426950408889634f;
-    PackedAttnArgs whole = a;
-    whole.parts = 1;
+template <typename T, int D>
+int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
+    PackedAttnArgs m = a;
+    m.parts = 1;
+    m.blocks = (int)packed_blocks(a, kPackedRowsMerge);
     HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
-    hipLaunchKernelGGL((packed_merge_kernel<T, D, ROWS>), packed_grid(whole), dim3(256), 0, st, a, c);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid(m), dim3(256), 0, st, m, a.parts, a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
     return hyb_check_launch("packed_attention_merge");
 }
 
-// How the keys are cut.  A launch whose row blocks would leave most of the chip idle (single tokens, the end of a long prompt) takes `parts` workgroups per
-// block, enough for every CU to hold its share, of at least 256 keys each.  max_k == 0: the keys of all sequences bound one sequence's.
-void choose_parts(PackedAttnArgs& a, int max_k, int head_dim, hyb_dtype dtype) {
-    a.parts = 1;
-    a.part_keys = 0;
-    const long long units = (long long)a.blocks * a.k_heads, slots = (long long)hyb_cu_count() * (dtype == HYB_BF16 && head_dim == 64 ? 4 : 2);
+// How the keys are cut: `parts` workgroups per block of rows, the same number of keys each, where a launch's row blocks would leave most of the chip idle (the end of a long prompt).
+// max_k == 0: the keys of all sequences bound one sequence's.
+void choose_parts(PackedAttnArgs& a, int max_k, int slots) {
+    const long long units = (long long)a.blocks * a.k_heads;
     const int keys = max_k > 0 && max_k < a.total_k ? max_k : a.total_k;
     if (units == 0 || units * 2 > slots || keys <= 512) return;
     long long parts = slots / units;
-    int len = (int)((keys + parts - 1) / parts);
-    len = (len + 63) / 64 * 64;
+    if (parts > kPackedMaxParts) parts = kPackedMaxParts;
+    long long len = ((keys + parts - 1) / parts + 63) / 64 * 64;
     if (len < 256) len = 256;
-    a.parts = (keys + len - 1) / len;
-    a.part_keys = len;
+    if (len >= keys) return;
+    a.parts = (int)((keys + len - 1) / len);
+    a.part_keys = (int)len;
+}
+// Pieces of the few-rows kernel: all keys dealt out over the chip, two pieces for every workgroup that fits it (one: 11 % slower over caches of 100 to 8000 keys, three: the same), of at
+// least 256 keys (8000 keys of one sequence, 8 heads of 128: 11.7 us; of 512: 13.0), or 512 where the sequences alone fill the chip.  Sequences of which the caller says that none is
+// longer than a piece are one piece each, whatever their length, and need no join.
+void choose_pieces(PackedAttnArgs& a, int max_k, int slots) {
+    long long len = ((long long)a.total_k * a.k_heads / (2 * slots) + 63) / 64 * 64;
+    const int least = (long long)a.sequences * a.k_heads >= slots ? 512 : 256;
+    if (len < least) len = least;
+    if (max_k > 0 && max_k <= len) len = 1 << 30;
+    a.part_keys = (int)len;
+    a.pieces = (int)(a.total_k / len) + a.sequences;
+    a.blocks = (int)packed_blocks(a, 1);       // of the join
 }
 
 int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttnArgs& a) {
@@ -295,17 +306,25 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     }
     a.q_token = d.q_token_stride * es; a.q_head = d.q_head_stride * es; a.k_token = d.k_token_stride * es; a.k_head = d.k_head_stride * es;
     a.v_token = d.v_token_stride * es; a.v_head = d.v_head_stride * es; a.o_token = d.o_token_stride * es; a.o_head = d.o_head_stride * es;
-    const int rows = d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim);
-    HYB_REQUIRE((long long)d.total_q * a.group < (1ll << 31) && packed_blocks(a, rows) * a.k_heads < (1ll << 27), HYB_ERR_SHAPE, "%s: too many queries (%d rows of %d heads)", who, d.total_q, d.q_heads);
-    a.blocks = (int)packed_blocks(a, rows);
+    HYB_REQUIRE(d.total_k <= 1 << 30, HYB_ERR_SHAPE, "%s: more than 2^30 rows of keys (%d)", who, d.total_k);
+    HYB_REQUIRE((long long)d.total_q * a.group < (1ll << 31) && packed_blocks(a, 1) * a.k_heads < (1ll << 31) && ((long long)d.total_k / 256 + d.sequences) * a.k_heads < (1ll << 29), HYB_ERR_SHAPE, "%s: too many rows (%d of queries, %d of keys, %d heads)", who, d.total_q, d.total_k, d.q_heads);
     a.xcd_heads = d.k_heads % 8 == 0 ? 8 : d.k_heads % 4 == 0 ? 4 : d.k_heads % 2 == 0 ? 2 : 1;
     a.xcd_share = 8 / a.xcd_heads;
-    choose_parts(a, d.max_k, d.head_dim, d.dtype);
+    a.parts = 1;
+    const int slots = hyb_cu_count() * (d.dtype == HYB_BF16 && d.head_dim == 64 ? 4 : 2);       // workgroups that the chip holds
+    // at most 16 rows per sequence: the kernel whose waves split the keys (only the sizes that the caller names can say so; any others are right, too)
+    if (d.dtype == HYB_BF16 && d.max_q > 0 && (long long)d.max_q * a.group <= kPackedRowsFew) {
+        choose_pieces(a, d.max_k, slots);
+    } else {
+        a.blocks = (int)packed_blocks(a, d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim));
+        choose_parts(a, d.max_k, slots);
+    }
     return HYB_OK;
 }
 
 size_t part_bytes(const PackedAttnArgs& a, int head_dim) {
-    return a.parts > 1 ? hyb_align_up(packed_part_floats(a.total_q, a.q_heads, a.parts, head_dim) * sizeof(float), 256) : 0;
+    const size_t floats = a.pieces > a.sequences ? packed_piece_rows(a.pieces, a.k_heads) * (head_dim + 2) : a.parts > 1 ? packed_part_floats(a.total_q, a.q_heads, a.parts, head_dim) : 0;
+    return hyb_align_up(floats * sizeof(float), 256);
 }
 
 }  // namespace
@@ -346,8 +365,8 @@ extern "C" int hyb_packed_attention(const hyb_packed_attention_desc* desc, const
     }
     a.q = q; a.k = k; a.v = v; a.o = o; a.offsets_q = offsets_q; a.offsets_k = offsets_k;
     const hipStream_t st = (hipStream_t)stream;
-    rc = d.dtype == HYB_BF16 ? hyb_launch_packed_attention_mfma(a, d.head_dim, st) : hyb_launch_packed_attention_f32(a, d.head_dim, st);
-    if (rc || a.parts == 1) return rc;
-    if (d.dtype == HYB_BF16) return d.head_dim == 64 ? launch_merge<bf16_t, 64, kPackedRowsMfma>(a, st) : launch_merge<bf16_t, 128, kPackedRowsMfma>(a, st);
-    return d.head_dim == 64 ? launch_merge<float, 64, packed_rows_f32(64)>(a, st) : launch_merge<float, 128, packed_rows_f32(128)>(a, st);
+    rc = a.pieces ? hyb_launch_packed_attention_few(a, d.head_dim, st) : d.dtype == HYB_BF16 ? hyb_launch_packed_attention_mfma(a, d.head_dim, st) : hyb_launch_packed_attention_f32(a, d.head_dim, st);
+    if (rc || a.pieces || a.parts == 1) return rc;
+    if (d.dtype == HYB_BF16) return d.head_dim == 64 ? launch_merge<bf16_t, 64>(a, st) : launch_merge<bf16_t, 128>(a, st);
+    return d.head_dim == 64 ? launch_merge<float, 64>(a, st) : launch_merge<float, 128>(a, st);
 }

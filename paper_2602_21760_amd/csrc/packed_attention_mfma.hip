@@ -39,8 +39,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-__device__ __forceinline__ bool not_finite(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
-
 // Transposing LDS reads of the V^T fragments of 32 output features (two 16-feature tiles, two 32-key steps of two reads each).  Written as asm so that they can be issued
 // ahead of their use: a wait that the compiler places before such a read through its builtin also waits for the next tile's copies.  Every result goes
 // through lds_wait(), which stands between these reads and their use and keeps the registers in use until they are written.
@@ -225,7 +223,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             for (int j = 0; j < TILE_BYTES / 1024; j++) {
                 const u32x4 x = *(const u32x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + j * 1024 + ln * 16);
 #pragma unroll
-                for (int e = 0; e < 4; e++) any |= ((x[e] & 0x7f80u) == 0x7f80u) | ((x[e] & 0x7f800000u) == 0x7f800000u);
+                for (int e = 0; e < 4; e++) any |= odd_bits_bf16(x[e]);
             }
             odd = __any(any != 0);
         }
@@ -305,9 +303,12 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
 #pragma unroll
                 for (int dd = 0; dd < 2; dd++)
 #pragma unroll
-                    for (int ks = 0; ks < 2; ks++)
+                    for (int ks = 0; ks < 2; ks++) {
+                        u32x4 w = __builtin_bit_cast(u32x4, vf[dd][ks]);
 #pragma unroll
-                        for (int j = 0; j < 8; j++) vf[dd][ks][j] = not_finite(vf[dd][ks][j]) ? (bf16_t)0.f : vf[dd][ks][j];
+                        for (int e = 0; e < 4; e++) w[e] &= ~odd_mask_bf16(w[e]);
+                        vf[dd][ks] = __builtin_bit_cast(bf16x8, w);
+                    }
             }
 #pragma unroll
             for (int dd = 0; dd < 2; dd++)
@@ -332,18 +333,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             const int ln = lane_again();
 #pragma unroll 1
             for (int key = 0; key < BKV; key++) {
-                bool seen[2];
+                unsigned seen[2];
 #pragma unroll
-                for (int qt = 0; qt < 2; qt++) seen[qt] = t * BKV + key <= row_last[wave * 32 + qt * 16 + ln % 16];
+                for (int qt = 0; qt < 2; qt++) seen[qt] = t * BKV + key <= row_last[wave * 32 + qt * 16 + ln % 16] ? ~0u : 0u;
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) {
-                    const bf16x4 x = *(const bf16x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + key * ROWB + (((2 * dt + ln / 32) ^ swz<D>(key)) * 16) + (ln / 16 % 2) * 8);
+                    const u32x2 x = *(const u32x2 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + key * ROWB + (((2 * dt + ln / 32) ^ swz<D>(key)) * 16) + (ln / 16 % 2) * 8);
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float add = not_finite(x[i]) ? (float)x[i] : 0.f;
-#pragma unroll
-                        for (int qt = 0; qt < 2; qt++) o[dt][qt][i] += seen[qt] ? add : 0.f;
-                    }
+                    for (int qt = 0; qt < 2; qt++) o[dt][qt] += only_odd(x, seen[qt]);
                 }
             }
         }

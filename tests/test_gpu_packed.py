@@ -298,6 +298,32 @@ def test_attention_hidden_keys_do_not_reach(hb, dt, d, bad):
     assert (np.abs(got - clean)[~dirty] <= bound[~dirty]).all()
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_hidden_keys_do_not_reach_few_queries(hb, dt, d, bad):
+    """The same for a few new tokens per sequence: the first of two does not see the last key."""
+    lq, lk = [2, 1, 2, 2], [70, 40, 900, 33]
+
+    def edit(q, k, v, cu_q, cu_k):
+        for x in (k, v):
+            x[:3] = bad
+            x[cu_k[-1]:] = bad
+        for s in (0, 2, 3):
+            v[cu_k[s + 1] - 1, :, 7] = bad
+        k[cu_k[1] - 1] = np.nan
+    got, want, inputs, same, _ = _attention(hb, dt, lq, lk, 6, 2, d, causal=True, spare=3, edit=edit)
+    q, k, v, cu_q, cu_k, causal, factor = inputs
+    assert same
+    dirty = np.zeros(len(got), dtype=bool)
+    dirty[[cu_q[1] - 1, cu_q[3] - 1, cu_q[4] - 1]] = True
+    assert not np.isfinite(got[dirty][:, :, 7]).any() and np.isfinite(got[cu_q[3] - 1][:, :7]).all()
+    k, v = (np.where(np.isfinite(x), x, 0.0) for x in (k, v))
+    clean = P.packed_attention(q, k, v, cu_q, cu_k, causal, factor, np.full(got.shape, 7.0))
+    bound = P.packed_attention_bound(q, k, v, cu_q, cu_k, dt == "bf16", causal, factor)
+    assert np.isfinite(got[~dirty]).all() and (np.abs(got - clean)[~dirty] <= bound[~dirty]).all()
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_values_seen_keep_their_infinity(hb, dt):
     """A value of +inf that a query sees makes that feature +inf, in a tile that not all rows see, and leaves the other features alone."""

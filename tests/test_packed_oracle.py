@@ -115,7 +115,7 @@ def _attention_desc(binding, **changes):
 @pytest.mark.parametrize("changes,code", [
     (dict(sequences=-1), 2), (dict(total_q=-1), 2), (dict(total_k=-1), 2), (dict(max_k=-1), 2), (dict(head_dim=32), 2), (dict(head_dim=96), 2), (dict(q_heads=3), 2), (dict(k_heads=0), 2),
     (dict(q_heads=0), 2), (dict(dtype=5), 3), (dict(q_token_stride=260), 4), (dict(v_head_stride=60), 4), (dict(k_token_stride=1 << 23), 2), (dict(k_head_stride=1 << 40), 2),
-    (dict(o_token_stride=192), 2), (dict(o_head_stride=56), 2), (dict(total_q=0x7fffffff), 2), (dict(q_heads=65536 * 2, k_heads=2), 2)])
+    (dict(o_token_stride=192), 2), (dict(o_head_stride=56), 2), (dict(total_q=0x7fffffff), 2), (dict(total_k=(1 << 30) + 1), 2), (dict(q_heads=65536 * 2, k_heads=2), 2)])
 def test_attention_refusals(lib, changes, code):
     from paper_2602_21760_amd import binding
     d = _attention_desc(binding, **changes)
