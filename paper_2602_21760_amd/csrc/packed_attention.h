@@ -90,11 +90,73 @@ __device__ __forceinline__ void packed_rows_of(const PackedAttnArgs& a, int s, P
     u.n_q = packed_offset(a.offsets_q, s + 1, a.total_q) - u.q0;
     u.n_k = max(packed_offset(a.offsets_k, s + 1, a.total_k) - u.k0, 0);
 }
+
+// Inclusive prefix sums and maxima over the wave, on the vector ALU alone: shifts inside rows of 16 lanes, then row totals handed upwards.
+__device__ __forceinline__ int packed_wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);    // row_bcast:15
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);    // row_bcast:31
+    return x;
+}
+__device__ __forceinline__ int packed_wave_total(int x) { return __builtin_amdgcn_readlane(packed_wave_prefix(x), 63); }
+__device__ __forceinline__ int packed_wave_max(int x) {               // of numbers >= 0
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The rank-th block in the order of decreasing numbers of keys: returns its index in its sequence (-1: there are fewer).  A launch takes several rounds of workgroups
+// of very different lengths, and ends when the last one does.  Lane s holds sequence s: how many of its blocks see at least w tiles of 64 keys has a closed
+// form (a causal sequence's later blocks see more), so the number of keys at that rank is found by bisection over w and the block by a prefix sum.  Fills in the
+// sequence's rows.
 template <int ROWS>
+__device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int rank, PackedUnit& u) {
+    const int lane = threadIdx.x % 64;
+    int q0 = 0, k0 = 0, n_q = 0, n_k = 0;
+    if (lane < a.sequences) {
+        q0 = packed_offset(a.offsets_q, lane, a.total_q);
+        k0 = packed_offset(a.offsets_k, lane, a.total_k);
+        n_q = max(packed_offset(a.offsets_q, lane + 1, a.total_q) - q0, 0);
+        n_k = max(packed_offset(a.offsets_k, lane + 1, a.total_k) - k0, 0);
+    }
+    const int rows = n_q * a.group, blocks = (int)(((unsigned)rows + ROWS - 1) / ROWS);
+    auto at_least = [&](int w) {      // blocks of the lane's sequence with w tiles or more
+        const int key = 64 * w - 63;                                       // w tiles: the last row sees this many keys
+        if (w == 0) return blocks;
+        if (n_k < key) return 0;
+        const int t = a.causal ? key - 1 - (n_k - n_q) : 0;                // the first query that does
+        return t <= 0 ? blocks : t >= n_q ? 0 : blocks - (int)((unsigned)(t * a.group) / ROWS);
+    };
+    if (rank >= packed_wave_total(blocks)) return -1;
+    int lo = 0, hi = packed_wave_max((n_k + 63) / 64) + 1;      // at_least(lo) in all is more than rank, at_least(hi) is not
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (packed_wave_total(at_least(mid)) > rank) lo = mid;
+        else hi = mid;
+    }
+    const int with = at_least(lo), more = at_least(hi), same = with - more;
+    const int below = packed_wave_prefix(same), e = rank - packed_wave_total(more);
+    const int s = __popcll(__ballot(below <= e)) & 63;       // the lane whose blocks hold it
+    u.sequence = s;
+    u.q0 = __builtin_amdgcn_readlane(q0, s);
+    u.k0 = __builtin_amdgcn_readlane(k0, s);
+    u.n_q = __builtin_amdgcn_readlane(n_q, s);
+    u.n_k = __builtin_amdgcn_readlane(n_k, s);
+    return __builtin_amdgcn_readlane(blocks - with + (e - (below - same)), s);
+}
+
+template <int ROWS, bool LONG_FIRST = false>
 __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
     PackedUnit u = {};
     // XCD x (workgroups go round to the 8 XCDs) serves key heads = x mod gcd(8, k_heads), and where XCDs share a head every 8 / gcd-th block of it: the keys of a
-    // head stay in as few L2s as possible, and every XCD gets blocks of all lengths.  Late blocks first: with a causal mask they are the long ones.
+    // head stay in as few L2s as possible, and every XCD gets blocks of all lengths.
     const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
     const int xcd = (int)(id % 8), hx = xcd % a.xcd_heads, sx = xcd / a.xcd_heads;
     unsigned j = id / 8;
@@ -103,13 +165,19 @@ __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
     if (u.head >= a.k_heads) return u;
     j %= per_head;
     u.part = (int)(j % (unsigned)a.parts);
-    const int block = a.blocks - 1 - ((int)(j / (unsigned)a.parts) * a.xcd_share + sx);
-    if (block < 0) return u;
-    const int s = packed_sequence_of(a.offsets_q, a.sequences, a.total_q, a.group, ROWS, block);
-    const int first = packed_first_piece(a.offsets_q, s, a.total_q, a.group, ROWS);
-    if (first > block) return u;
-    packed_rows_of(a, s, u);
-    u.sequence = s;
+    int block = (int)(j / (unsigned)a.parts) * a.xcd_share + sx;
+    if (block >= a.blocks) return u;
+    int first = 0;
+    if (LONG_FIRST && a.sequences > 1 && a.sequences <= 64) {
+        block = packed_ranked_block<ROWS>(a, block, u);
+        if (block < 0) return u;
+    } else {
+        block = a.blocks - 1 - block;        // late blocks first: with a causal mask they are the long ones
+        u.sequence = packed_sequence_of(a.offsets_q, a.sequences, a.total_q, a.group, ROWS, block);
+        first = packed_first_piece(a.offsets_q, u.sequence, a.total_q, a.group, ROWS);
+        if (first > block) return u;
+        packed_rows_of(a, u.sequence, u);
+    }
     const long long all = (long long)max(u.n_q, 0) * a.group, row0 = (long long)(block - first) * ROWS;
     u.rows = (int)max(min(all - row0, (long long)ROWS), 0ll);
     u.row0 = (int)row0;           // (meaningful when rows > 0: below total_q * group, which the launcher keeps below 2^31)

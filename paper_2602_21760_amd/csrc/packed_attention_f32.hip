@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
     constexpr int BQ = packed_rows_f32(D), QT = BQ / 16, DT = D / 16, VH = D / 64;
     __shared__ float part_o[WAVES][QT][DT][4][64];   // [wave][row tile][feature tile][register][lane]
     __shared__ float part_ml[WAVES][QT][2][16];      // [wave][row tile][maximum, normaliser][row]
-    const PackedUnit u = packed_unit<BQ>(a);
+    const PackedUnit u = packed_unit<BQ, true>(a);
     if (u.rows == 0) return;
     const int lane = threadIdx.x % 64, l16 = lane % 16, q4 = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);

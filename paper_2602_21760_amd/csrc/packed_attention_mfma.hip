@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
     __shared__ __attribute__((aligned(4 * TILE_BYTES))) unsigned char smem[2][2 * TILE_BYTES];
     __shared__ int row_last[BQ];         // last key that each row sees (read in masked tiles only)
 
-    const PackedUnit u = packed_unit<BQ>(a);
+    const PackedUnit u = packed_unit<BQ, true>(a);
     if (u.rows == 0) return;
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
