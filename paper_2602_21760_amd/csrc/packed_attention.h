@@ -6,12 +6,25 @@
 #pragma once
 #include "common.h"
 
+// n / d for 0 <= n < 2^32 by a multiplication and shifts (l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1: the quotient is exact).
+struct PackedDivisor { unsigned m, shift1, shift2; };
+inline PackedDivisor packed_divisor(unsigned d) {
+    unsigned l = 0;
+    while (l < 32 && ((unsigned long long)1 << l) < d) l++;
+    return {(unsigned)((((unsigned long long)1 << l) - d) * ((unsigned long long)1 << 32) / d) + 1, l < 1 ? l : 1, l > 1 ? l - 1 : 0};
+}
+__device__ __forceinline__ int packed_div(int n, PackedDivisor d) {
+    const unsigned t = __umulhi(d.m, (unsigned)n);
+    return (int)((t + (((unsigned)n - t) >> d.shift1)) >> d.shift2);
+}
+
 struct PackedAttnArgs {
     const void *q, *k, *v;
     void* o;
     const int *offsets_q, *offsets_k;
     int sequences, total_q, total_k;
     int q_heads, k_heads, group;
+    PackedDivisor by_group;
     float scale;                                  // > 0; PRE kernels do not use it
     int causal, prescaled;
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
@@ -49,9 +62,11 @@ inline dim3 packed_grid_of(size_t total) {
     const size_t x = total < ((size_t)1 << 23) ? total : (size_t)1 << 23;
     return dim3((unsigned)x, (unsigned)((total + x - 1) / x));
 }
-inline dim3 packed_grid(const PackedAttnArgs& a) {
-    return packed_grid_of(8 * (size_t)(a.k_heads / a.xcd_heads) * ((a.blocks + a.xcd_share - 1) / a.xcd_share) * a.parts);
+__host__ __device__ inline unsigned packed_units(const PackedAttnArgs& a) {
+    return 8u * (unsigned)(a.k_heads / a.xcd_heads) * (unsigned)((a.blocks + a.xcd_share - 1) / a.xcd_share) * (unsigned)a.parts;
 }
+inline dim3 packed_grid(const PackedAttnArgs& a) { return packed_grid_of(packed_units(a)); }
+__device__ __forceinline__ unsigned packed_group_id() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 // Rows of a sequence after the offsets are brought into 0 .. total.
 __device__ __forceinline__ int packed_offset(const int* offsets, int s, int total) { return min(max(offsets[s], 0), total); }
@@ -91,31 +106,10 @@ __device__ __forceinline__ void packed_rows_of(const PackedAttnArgs& a, int s, P
     u.n_k = max(packed_offset(a.offsets_k, s + 1, a.total_k) - u.k0, 0);
 }
 
-// Inclusive prefix sums and maxima over the wave, on the vector ALU alone: shifts inside rows of 16 lanes, then row totals handed upwards.
-__device__ __forceinline__ int packed_wave_prefix(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // row_shr:1
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);    // row_bcast:15
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);    // row_bcast:31
-    return x;
-}
-__device__ __forceinline__ int packed_wave_total(int x) { return __builtin_amdgcn_readlane(packed_wave_prefix(x), 63); }
-__device__ __forceinline__ int packed_wave_max(int x) {               // of numbers >= 0
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
-// The rank-th block in the order of decreasing numbers of keys: returns its index in its sequence (-1: there are fewer).  A launch takes several rounds of workgroups
-// of very different lengths, and ends when the last one does.  Lane s holds sequence s: how many of its blocks see at least w tiles of 64 keys has a closed
-// form (a causal sequence's later blocks see more), so the number of keys at that rank is found by bisection over w and the block by a prefix sum.  Fills in the
-// sequence's rows.
+// The rank-th block when sequences come in the order of decreasing numbers of keys (up to 64 of them) and a sequence's late blocks first, which are the long ones
+// with a causal mask: a launch takes several rounds of workgroups of very different lengths and ends when the last one does.  Lane s holds sequence s and counts the
+// blocks before its own.  Fills in the sequence's rows; returns the block's index in its sequence (-1: there are fewer).  (The order of single blocks by their number of
+// keys, by bisection, takes three times the instructions and no less time; a table of it made by a kernel before this one neither.)
 template <int ROWS>
 __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int rank, PackedUnit& u) {
     const int lane = threadIdx.x % 64;
@@ -126,38 +120,27 @@ __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int 
         n_q = max(packed_offset(a.offsets_q, lane + 1, a.total_q) - q0, 0);
         n_k = max(packed_offset(a.offsets_k, lane + 1, a.total_k) - k0, 0);
     }
-    const int rows = n_q * a.group, blocks = (int)(((unsigned)rows + ROWS - 1) / ROWS);
-    auto at_least = [&](int w) {      // blocks of the lane's sequence with w tiles or more
-        const int key = 64 * w - 63;                                       // w tiles: the last row sees this many keys
-        if (w == 0) return blocks;
-        if (n_k < key) return 0;
-        const int t = a.causal ? key - 1 - (n_k - n_q) : 0;                // the first query that does
-        return t <= 0 ? blocks : t >= n_q ? 0 : blocks - (int)((unsigned)(t * a.group) / ROWS);
-    };
-    if (rank >= packed_wave_total(blocks)) return -1;
-    int lo = 0, hi = packed_wave_max((n_k + 63) / 64) + 1;      // at_least(lo) in all is more than rank, at_least(hi) is not
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (packed_wave_total(at_least(mid)) > rank) lo = mid;
-        else hi = mid;
-    }
-    const int with = at_least(lo), more = at_least(hi), same = with - more;
-    const int below = packed_wave_prefix(same), e = rank - packed_wave_total(more);
-    const int s = __popcll(__ballot(below <= e)) & 63;       // the lane whose blocks hold it
+    const int blocks = (int)(((unsigned)(n_q * a.group) + ROWS - 1) / ROWS);
+    const int key = min(n_k, (1 << 24) - 1) * 64 + 63 - lane;       // all different
+    int before = 0;
+    for (int s = 0; s < a.sequences; s++) before += __builtin_amdgcn_readlane(key, s) > key ? __builtin_amdgcn_readlane(blocks, s) : 0;
+    const unsigned long long here = __ballot(rank >= before && rank - before < blocks);
+    if (here == 0) return -1;
+    const int s = __builtin_ctzll(here);
     u.sequence = s;
     u.q0 = __builtin_amdgcn_readlane(q0, s);
     u.k0 = __builtin_amdgcn_readlane(k0, s);
     u.n_q = __builtin_amdgcn_readlane(n_q, s);
     u.n_k = __builtin_amdgcn_readlane(n_k, s);
-    return __builtin_amdgcn_readlane(blocks - with + (e - (below - same)), s);
+    return __builtin_amdgcn_readlane(blocks - 1 - (rank - before), s);
 }
 
+// Unit number `id` of a launch; there are packed_units(a), most of them with rows.
 template <int ROWS, bool LONG_FIRST = false>
-__device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a) {
+__device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a, unsigned id) {
     PackedUnit u = {};
     // XCD x (workgroups go round to the 8 XCDs) serves key heads = x mod gcd(8, k_heads), and where XCDs share a head every 8 / gcd-th block of it: the keys of a
     // head stay in as few L2s as possible, and every XCD gets blocks of all lengths.
-    const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
     const int xcd = (int)(id % 8), hx = xcd % a.xcd_heads, sx = xcd / a.xcd_heads;
     unsigned j = id / 8;
     const unsigned per_head = (unsigned)((a.blocks + a.xcd_share - 1) / a.xcd_share) * (unsigned)a.parts;

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
     constexpr int BQ = packed_rows_f32(D), QT = BQ / 16, DT = D / 16, VH = D / 64;
     __shared__ float part_o[WAVES][QT][DT][4][64];   // [wave][row tile][feature tile][register][lane]
     __shared__ float part_ml[WAVES][QT][2][16];      // [wave][row tile][maximum, normaliser][row]
-    const PackedUnit u = packed_unit<BQ, true>(a);
+    const PackedUnit u = packed_unit<BQ, true>(a, packed_group_id());
     if (u.rows == 0) return;
     const int lane = threadIdx.x % 64, l16 = lane % 16, q4 = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -35,13 +35,13 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
     int last[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; qt++) {
-        const int row = u.row0 + min(qt * 16 + l16, u.rows - 1), t = row / a.group;
+        const int row = u.row0 + min(qt * 16 + l16, u.rows - 1), t = packed_div(row, a.by_group);
         last[qt] = packed_last_key(a, u, t);
         const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + row - t * a.group) * a.q_head;
 #pragma unroll
         for (int s = 0; s < DT; s++) q[qt][s] = *reinterpret_cast<const f32x4*>(qp + 64 * s + 16 * q4);
     }
-    const int block_min = packed_last_key(a, u, u.row0 / a.group), block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
+    const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group)), block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
     const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;
     const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
     const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 #pragma unroll
                 for (int e = 0; e < 4; e++) r[h][e] = fmaf(part_o[p][qt][4 * h + e][wave][lane], w, r[h][e]);
         }
-        const int row = u.row0 + qt * 16 + l16, tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+        const int row = u.row0 + qt * 16 + l16, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
         if (a.parts > 1) {
             const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
             if (q4 == 0 && wave == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{m_all, l_all};
@@ -213,10 +213,10 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 template <typename T, int D>
 __global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, int parts, float c) {
     constexpr int N = D / 64;
-    const PackedUnit u = packed_unit<kPackedRowsMerge>(a);
+    const PackedUnit u = packed_unit<kPackedRowsMerge>(a, packed_group_id());
     const int lane = threadIdx.x % 64, r = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     if (r >= u.rows) return;
-    const int row = u.row0 + r, tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+    const int row = u.row0 + r, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
     const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * parts;
     const float* o = a.part + at * D + lane * N;
     f32x2 ml = {-__builtin_inff(), 0.f};
@@ -298,6 +298,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     a = {};
     a.sequences = d.sequences; a.total_q = d.total_q; a.total_k = d.total_k;
     a.q_heads = d.q_heads; a.k_heads = d.k_heads; a.group = d.q_heads / d.k_heads;
+    a.by_group = packed_divisor((unsigned)a.group);
     a.scale = d.scale > 0.f ? d.scale : (d.head_dim == 64 ? 0.125f : 0.08838834764831845f);
     a.causal = d.causal != 0; a.prescaled = d.prescaled != 0;
     if (a.prescaled && d.dtype == HYB_F32) {      // the fp32 kernel exponentiates scale x score in base e
@@ -322,7 +323,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     return HYB_OK;
 }
 
-size_t part_bytes(const PackedAttnArgs& a, int head_dim) {
+size_t scratch_bytes(const PackedAttnArgs& a, int head_dim) {
     const size_t floats = a.pieces > a.sequences ? packed_piece_rows(a.pieces, a.k_heads) * (head_dim + 2) : a.parts > 1 ? packed_part_floats(a.total_q, a.q_heads, a.parts, head_dim) : 0;
     return hyb_align_up(floats * sizeof(float), 256);
 }
@@ -339,7 +340,7 @@ int hyb_launch_packed_attention_f32(const PackedAttnArgs& a, int head_dim, hipSt
 extern "C" size_t hyb_packed_attention_workspace_bytes(const hyb_packed_attention_desc* desc) {
     PackedAttnArgs a;
     if (fill_args("hyb_packed_attention_workspace_bytes", desc, a) != HYB_OK) return 0;
-    return part_bytes(a, desc->head_dim);
+    return scratch_bytes(a, desc->head_dim);
 }
 
 extern "C" int hyb_packed_attention(const hyb_packed_attention_desc* desc, const void* q, const void* k, const void* v, void* o,
@@ -357,7 +358,7 @@ extern "C" int hyb_packed_attention(const hyb_packed_attention_desc* desc, const
     HYB_REQUIRE((d.o_head_stride >= row && d.o_token_stride >= (heads - 1) * d.o_head_stride + row) ||
                     (d.o_token_stride >= row && d.o_head_stride >= ((size_t)d.total_q - 1) * d.o_token_stride + row),
                 HYB_ERR_SHAPE, "hyb_packed_attention: the strides of o let its rows overlap");
-    const size_t need = part_bytes(a, d.head_dim);
+    const size_t need = scratch_bytes(a, d.head_dim);
     if (need > 0) {
         HYB_CHECK_PTR(workspace); HYB_CHECK_ALIGN(workspace);
         HYB_REQUIRE(workspace_bytes >= need, HYB_ERR_WORKSPACE, "hyb_packed_attention: workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
     __shared__ float part_ml[WAVES][2][BQ];
     PackedUnit u = {};
     // XCD x serves the key heads = x mod gcd(8, k_heads), see packed_unit()
-    const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
+    const unsigned id = packed_group_id();
     const int xcd = (int)(id % 8), per_head = (a.pieces + a.xcd_share - 1) / a.xcd_share;
     u.head = xcd % a.xcd_heads + a.xcd_heads * (int)(id / 8 / (unsigned)per_head);
     const int piece = (int)(id / 8 % (unsigned)per_head) * a.xcd_share + xcd / a.xcd_heads;
@@ -98,14 +98,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
     for (u.row0 = 0; u.row0 < rows; u.row0 += BQ) {
         u.rows = min(rows - u.row0, BQ);
         if (u.row0 > 0) __syncthreads();       // everyone is done with the last block's results
-        const int row = u.row0 + min(l16, u.rows - 1), tok = row / a.group, last = packed_last_key(a, u, tok);
+        const int row = u.row0 + min(l16, u.rows - 1), tok = packed_div(row, a.by_group), last = packed_last_key(a, u, tok);
         bf16x8 qf[KS];
         {
             const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + tok) * a.q_token + (size_t)(u.head * a.group + row - tok * a.group) * a.q_head;
 #pragma unroll
             for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 64 + kq * 16);
         }
-        const int block_min = packed_last_key(a, u, u.row0 / a.group), block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
+        const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group)), block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
         const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;
         const int t_begin = parts > 1 ? min(u.part * part_tiles, nt) : 0, t_end = parts > 1 ? min(t_begin + part_tiles, nt) : nt;
 
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
 #pragma unroll
                 for (int e = 0; e < 4; e++) x[e] = fmaf(y[e], w, x[e]);
             }
-            const int rr = u.row0 + r, tk = rr / a.group, head = u.head * a.group + (rr - tk * a.group);
+            const int rr = u.row0 + r, tk = packed_div(rr, a.by_group), head = u.head * a.group + (rr - tk * a.group);
             if (parts > 1) {
                 const size_t at = ((size_t)piece * a.k_heads + u.head) * BQ + r;
                 if (f == 0) *reinterpret_cast<f32x2*>(a.part + packed_piece_rows(a.pieces, a.k_heads) * D + at * 2) = f32x2{m_all, l};
@@ -255,12 +255,12 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttnArgs a, floa
     constexpr int F = D / 4, G = 256 / F, U = 64 / G;
     __shared__ f32x4 sums[G][F];
     __shared__ float weight[64];
-    const PackedUnit u = packed_unit<1>(a);
+    const PackedUnit u = packed_unit<1>(a, packed_group_id());
     if (u.rows == 0 || u.n_q * a.group > BQ) return;
     const int parts = (u.n_k + a.part_keys - 1) / a.part_keys;
     if (parts <= 1) return;              // (written already)
     const int tid = threadIdx.x, f = tid % F, g = tid / F;
-    const int row = u.row0, tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+    const int row = u.row0, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
     const size_t at = ((size_t)packed_first_piece(a.offsets_k, u.sequence, a.total_k, 1, a.part_keys) * a.k_heads + u.head) * BQ + row, step = (size_t)a.k_heads * BQ;
     const f32x2* ml = reinterpret_cast<const f32x2*>(a.part + packed_piece_rows(a.pieces, a.k_heads) * D) + at;
     const float* o = a.part + at * D + 4 * f;

@@ -13,8 +13,9 @@
 // Probabilities are rounded to bf16 for the second contraction and the normaliser is the sum of the rounded ones.
 //
 // Masks: the last key that a row sees is one number per row (causal, or the end of the sequence); only tiles in which a wave's rows differ from
-// "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA, so such a tile is
-// searched for them first, and if there are any they are zeroed in the fragments and added to the rows that see them.
+// "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA.  The first attempt lets them in; if a
+// result is not finite, the workgroup starts over in the same way as for sums out of range, and the second attempt searches every tile that not all rows see, zeroes such
+// values in the fragments and adds them to the rows that do see them.  (The search in the first attempt takes 3 to 9 % of launches over short sequences.)
 #include "packed_attention.h"
 
 #include <type_traits>
@@ -99,8 +100,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
     // [buffer][K tile | V tile]
     __shared__ __attribute__((aligned(4 * TILE_BYTES))) unsigned char smem[2][2 * TILE_BYTES];
     __shared__ int row_last[BQ];         // last key that each row sees (read in masked tiles only)
+    __shared__ int wave_flags[4];
 
-    const PackedUnit u = packed_unit<BQ, true>(a);
+    const PackedUnit u = packed_unit<BQ, true>(a, packed_group_id());
     if (u.rows == 0) return;
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
 #pragma unroll
     for (int qt = 0; qt < 2; qt++) {
         const int row = u.row0 + min(wave * 32 + qt * 16 + l16, u.rows - 1);
-        const int t = row / a.group, g = row - t * a.group;
+        const int t = packed_div(row, a.by_group), g = row - t * a.group;
         if (q4 == 0) row_last[wave * 32 + qt * 16 + l16] = packed_last_key(a, u, t);
         const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + g) * a.q_head;
 #pragma unroll
@@ -120,15 +122,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
     }
     // the wave's rows see at least the keys 0 .. wave_min and at most 0 .. wave_max, the block's rows at most 0 .. block_max
     const bool active = wave * 32 < u.rows;
-    const int wave_min = packed_last_key(a, u, (u.row0 + min(wave * 32, u.rows - 1)) / a.group);
-    const int wave_max = active ? packed_last_key(a, u, (u.row0 + min(wave * 32 + 31, u.rows - 1)) / a.group) : -1;
-    const int block_max = packed_last_key(a, u, (u.row0 + u.rows - 1) / a.group);
+    const int wave_min = packed_last_key(a, u, packed_div(u.row0 + min(wave * 32, u.rows - 1), a.by_group));
+    const int wave_max = active ? packed_last_key(a, u, packed_div(u.row0 + min(wave * 32 + 31, u.rows - 1), a.by_group)) : -1;
+    const int block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
 
     const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;                    // (block_max == -1: no tile)
     const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
     const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
     // Tiles t_begin .. plain_end - 1 are seen whole by all rows and followed by a tile of 64 keys: a loop of its own, which holds no masks in registers.
-    const int block_min = packed_last_key(a, u, u.row0 / a.group);
+    const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group));
     const int plain_end = min(min((block_min + 1) / BKV, u.n_k / BKV - 1), t_end - 1);
 
     // Tile copy: lane i of a 1 KB chunk fills slot i % SLOTS of row i / SLOTS with feature vector slot ^ swz(row) (the swizzle is the same for a wave's
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
         });
 
         bf16x4 vh[2][2][2][2];   // [two groups of 32 features in flight][16-feature tile][32-key step][read]
-        bool odd = false;        // infinities or NaN among the values of a tile that not all rows see
+        bool odd = false;        // infinities or NaN among the values of a tile that not all rows see (looked for in the second attempt only)
         if (masked) {
             const int ln = lane_again();
 #pragma unroll
@@ -218,14 +220,16 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
                     for (int i = 0; i < 4; i++)
                         if (kt * 16 + i > seen) s[kt][qt][i] = -__builtin_inff();
             }
-            unsigned any = 0;
+            if constexpr (!DIRECT) {
+                unsigned any = 0;
 #pragma unroll 1
-            for (int j = 0; j < TILE_BYTES / 1024; j++) {
-                const u32x4 x = *(const u32x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + j * 1024 + ln * 16);
+                for (int j = 0; j < TILE_BYTES / 1024; j++) {
+                    const u32x4 x = *(const u32x4 __attribute__((address_space(3)))*)(lds0 + (buf ? OTHER : 0u) + TILE_BYTES + j * 1024 + ln * 16);
 #pragma unroll
-                for (int e = 0; e < 4; e++) any |= odd_bits_bf16(x[e]);
+                    for (int e = 0; e < 4; e++) any |= odd_bits_bf16(x[e]);
+                }
+                odd = __any(any != 0);
             }
-            odd = __any(any != 0);
         }
         if constexpr (DIRECT) v_reads<D>(vb, vh[0]);       // (the form with row maxima holds more values meanwhile and requests them after them)
         // the exponentiated scores of key tiles 2 ks, 2 ks + 1, rounded to bf16, are the B operand of 32-key step ks
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             } else {
                 lds_wait<0>(vh[g & 1], vf);
             }
-            if (odd) {
+            if (!DIRECT && odd) {
 #pragma unroll
                 for (int dd = 0; dd < 2; dd++)
 #pragma unroll
@@ -329,7 +333,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
                         }
             }
         }
-        if (odd) {
+        if (!DIRECT && odd) {
             const int ln = lane_again();
 #pragma unroll 1
             for (int key = 0; key < BKV; key++) {
@@ -379,13 +383,19 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             // (a row that sees none of these keys has no sum to judge)
             if (active && t_begin < t_end && row_last[wave * 32 + qt * 16 + lane_again() % 16] >= t_begin * BKV) out_of_range |= !(l > 0x1p-64f && l < 0x1p+64f);       // also true for NaN
         }
+        // an infinity or NaN in a row's result may come from a value that the row does not see (0 x it in an MFMA); 0 x the results finds them
+        f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int qt = 0; qt < 2; qt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) zero[i] = fmaf(o[dt][qt][i], 0.f, zero[i]);
+        out_of_range |= !(zero[0] + zero[1] + zero[2] + zero[3] == 0.f);
         const int wave_bad = __any(out_of_range) ? 1 : 0;
-        __syncthreads();                                     // every wave is done with the tile buffers
-        volatile int* flags = reinterpret_cast<volatile int*>(&smem[0][0]);
-        if (lane == 0) flags[wave] = wave_bad;
-        __syncthreads();
-        const bool again = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
-        __syncthreads();                                     // the flags are read before the buffers are refilled
+        if (lane == 0) wave_flags[wave] = wave_bad;
+        __syncthreads();                                     // ... and every wave is done with the tile buffers
+        const bool again = (wave_flags[0] | wave_flags[1] | wave_flags[2] | wave_flags[3]) != 0;
         if (again) {
             clear(-__builtin_inff());
             key_loop(std::false_type{});
@@ -398,7 +408,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
         const float l = row_total(l_run[qt]);
         if (wave * 32 + qt * 16 + l16e >= u.rows) continue;
         const int row = u.row0 + wave * 32 + qt * 16 + l16e;
-        const int tok = row / a.group, head = u.head * a.group + (row - tok * a.group);
+        const int tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
         if (a.parts > 1) {
             const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
             if (q4e == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
