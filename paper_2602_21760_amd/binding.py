@@ -424,6 +424,9 @@ def hyb_convert(src, out):
     return out
 
 
+_shape_of, _stride_of, _device_of, _address_of = operator.attrgetter("shape"), torch.Tensor.stride, torch.Tensor.get_device, torch.Tensor.data_ptr
+
+
 def _here(*tensors):
     """The tensors (None among them) live on the current device, whose stream the call goes to."""
     device = torch._C._cuda_getDevice()
@@ -432,20 +435,58 @@ def _here(*tensors):
             raise ValueError("tensor on %s, but the current device is cuda:%d" % (t.device, device))
 
 
+def _like(*tensors):
+    """How tensors are laid out: their shapes, strides and types."""
+    return [*map(_shape_of, tensors)], [*map(_stride_of, tensors)], [*map(_dtype_of, tensors)]
+
+
+def _addresses(tensors, like, names):
+    """(device, device pointers) of the tensors of a call, which must be on the current device and laid out as `like` says.  (One pass per property: a small call is bound by
+    the host, and this costs a third of looking at one tensor after the other.)"""
+    device = torch._C._cuda_getDevice()
+    try:
+        if ([*map(_shape_of, tensors)] == like[0] and [*map(_stride_of, tensors)] == like[1] and [*map(_dtype_of, tensors)] == like[2] and
+                [*map(_device_of, tensors)].count(device) == len(tensors)):
+            return device, [*map(_address_of, tensors)]
+    except (AttributeError, TypeError):         # None, or no tensor at all, among them
+        pass
+    for t, name, shape, stride, dtype in zip(tensors, names, *like):
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype:
+            raise ValueError("%s must be a tensor of shape %s and type %s" % (name, tuple(shape), dtype))
+        # (strides of axes of one element say nothing, and none do if there are no elements)
+        if t.numel() and any(x != y for x, y, n in zip(t.stride(), stride, shape) if n != 1):
+            raise ValueError("%s must have the strides %s" % (name, stride))
+    _here(*tensors)
+    return device, [*map(_address_of, tensors)]
+
+
+def _contiguous(*shape):
+    """(shape, strides) of a contiguous tensor."""
+    strides, step = [], 1
+    for n in reversed(shape):
+        strides.insert(0, step)
+        step *= max(n, 1)
+    return shape, tuple(strides)
+
+
+_LAYOUT_NAMES = ("shapes", "offsets", "request", "positions")
+
+
 def hyb_packed_layout(shapes, offsets, request=None, positions=None, text_after=False):
     """shapes: int32[requests, 4] = (frames, height, width, text tokens); offsets: int32[requests + 1]; request: int32[rows], positions: int32[rows, 3],
     or None; rows is the capacity."""
-    if shapes.dim() != 2 or shapes.shape[1] != 4 or offsets.dim() != 1 or offsets.shape[0] != shapes.shape[0] + 1:
-        raise ValueError("shapes must be [requests, 4] and offsets [requests + 1]")
-    if (request is not None and request.dim() != 1) or (positions is not None and (positions.dim() != 2 or positions.shape[1] != 3)):
-        raise ValueError("request must be [rows] and positions [rows, 3]")
-    rows = {t.shape[0] for t in (request, positions) if t is not None}
-    if len(rows) > 1:
-        raise ValueError("request and positions must have the same number of rows")
-    args = _p(shapes, torch.int32), _p(offsets, torch.int32), _p(request, torch.int32), _p(positions, torch.int32)
-    _here(shapes, offsets, request, positions)
-    # (offsets alone: nothing is cut off)
-    _check(lib().hyb_packed_layout(args[0], shapes.shape[0], rows.pop() if rows else 0x7fffffff, bool(text_after), args[1], args[2], args[3], _stream()))
+    n = shapes.shape[0]
+    rows = request.shape[0] if request is not None else positions.shape[0] if positions is not None else 0x7fffffff     # (offsets alone: nothing is cut off)
+    int32 = torch.int32
+    if request is not None and positions is not None:
+        device, (ps, po, pr, pp) = _addresses((shapes, offsets, request, positions), ([(n, 4), (n + 1,), (rows,), (rows, 3)], [(4, 1), (1,), (1,), (3, 1)], [int32] * 4), _LAYOUT_NAMES)
+    else:
+        given = [(t, name, _contiguous(*s)) for t, name, s in zip((shapes, offsets, request, positions), _LAYOUT_NAMES, ((n, 4), (n + 1,), (rows,), (rows, 3))) if t is not None]
+        device, found = _addresses([g[0] for g in given], ([g[2][0] for g in given], [g[2][1] for g in given], [int32] * len(given)), [g[1] for g in given])
+        ps, po, pr, pp = found[0], found[1], found[2] if request is not None else None, found[2] if positions is not None else None
+    rc = lib().hyb_packed_layout(ps, n, rows, 1 if text_after else 0, po, pr, pp, torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc)
     return offsets
 
 
@@ -458,23 +499,15 @@ def _head_strides(t, name):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * head, t.shape[1] * t.shape[2]), head
 
 
-def _like(t):
-    return t.shape, t.stride(), t.dtype
-
-
-def _checked(desc, tensors):
-    """Device pointers of the tensors of a call (None -> NULL); they must be laid out as those that the descriptor was made from."""
-    device, out = torch._C._cuda_getDevice(), []
-    for t, like in zip(tensors, desc.like):
-        if like is None:
-            out.append(None)
-            continue
-        if t is None or (t.shape, t.stride(), t.dtype) != like:
-            raise ValueError("a tensor differs in shape, strides or type from the one that the descriptor was made from")
-        if t.get_device() != device:
-            raise ValueError("tensor on %s, but the current device is cuda:%d" % (t.device, device))
-        out.append(t.data_ptr())
-    return out
+def _with_ints(tensors, *int_shapes):
+    """_like of the tensors and of contiguous int32 tensors behind them."""
+    shapes, strides, dtypes = _like(*tensors)
+    for s in int_shapes:
+        shape, stride = _contiguous(*s)
+        shapes.append(shape)
+        strides.append(stride)
+        dtypes.append(torch.int32)
+    return shapes, strides, dtypes
 
 
 def rotary_desc(q, k, axis_dims, theta=10000.0, pairs=HYB_ROTARY_NEIGHBOURS, axis_scale=None, q_scale=1.0, inverse=False, q_out=None, k_out=None):
@@ -501,19 +534,27 @@ def rotary_desc(q, k, axis_dims, theta=10000.0, pairs=HYB_ROTARY_NEIGHBOURS, axi
             strides.append(token)
     desc = RotaryDesc(q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], axes, (C.c_int * 4)(*axis_dims), (C.c_float * 4)(*(axis_scale or ())),
                       theta, pairs, int(inverse), q_scale, _dt(q), strides[0], strides[2], strides[1], strides[3])
-    desc.like = _like(q), k if k is None else _like(k), _like(q if q_out is None else q_out), k if k is None else _like(k if k_out is None else k_out)
+    tensors = (q, q if q_out is None else q_out) if k is None else (q, q if q_out is None else q_out, k, k if k_out is None else k_out)
+    desc.like = _with_ints(tensors, (desc.tokens, axes))
     return desc
 
 
 def hyb_rotary(desc, positions, q, k=None, q_out=None, k_out=None):
     """positions: int32[tokens, axes]; q, k, q_out, k_out as desc was made (None: in place)."""
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    if positions.shape != (desc.tokens, desc.axes):
-        raise ValueError("positions must be [%d, %d]" % (desc.tokens, desc.axes))
-    p = _p(positions, torch.int32)
-    _here(positions)
-    pq, pk, pqo, pko = _checked(desc, (q, k, q_out, k_out))
-    _check(lib().hyb_rotary(C.byref(desc), p, pq, pqo, pk, pko, _stream()))
+    if q_out is None:
+        q_out = q
+    if k_out is None:
+        k_out = k
+    if desc.k_heads or len(desc.like[0]) == 5:
+        device, (pq, pqo, pk, pko, pos) = _addresses((q, q_out, k, k_out, positions), desc.like, ("q", "q_out", "k", "k_out", "positions"))
+    elif k is not None or k_out is not None:
+        raise ValueError("the descriptor was made without k")
+    else:
+        device, (pq, pqo, pos) = _addresses((q, q_out, positions), desc.like, ("q", "q_out", "positions"))
+        pk = pko = None
+    rc = lib().hyb_rotary(desc, pos, pq, pqo, pk, pko, torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc)
     return q_out, k_out
 
 
@@ -529,23 +570,29 @@ def packed_attention_desc(q, k, v, o, offsets_q, max_q=0, max_k=0, causal=False,
     strides = [s for t, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o")) for s in _head_strides(t, n)]
     desc = PackedAttentionDesc(offsets_q.shape[0] - 1, q.shape[0], k.shape[0], max_q, max_k, q.shape[1], k.shape[1], q.shape[2], scale, int(causal), int(prescaled),
                                _dt(q), *strides)
-    desc.like = _like(q), _like(k), _like(v), _like(o)
+    desc.like = _with_ints((q, k, v, o), (desc.sequences + 1,), (desc.sequences + 1,))
     return desc
 
 
 def hyb_packed_attention_workspace_bytes(desc):
-    return lib().hyb_packed_attention_workspace_bytes(C.byref(desc))
+    return lib().hyb_packed_attention_workspace_bytes(desc)
+
+
+_ATTENTION_NAMES = ("q", "k", "v", "o", "offsets_q", "offsets_k")
 
 
 def hyb_packed_attention(desc, q, k, v, o, offsets_q, offsets_k, workspace=None):
     """q, k, v, o as desc was made; offsets_q, offsets_k: int32[sequences + 1]; workspace: torch.uint8 tensor of hyb_packed_attention_workspace_bytes(desc),
     or None if that is 0."""
-    if offsets_q.shape != (desc.sequences + 1,) or offsets_k.shape != offsets_q.shape:
-        raise ValueError("offsets must be [%d]" % (desc.sequences + 1))
-    cq, ck, ws = _p(offsets_q, torch.int32), _p(offsets_k, torch.int32), _p(workspace)
-    _here(offsets_q, offsets_k, workspace)
-    pq, pk, pv, po = _checked(desc, (q, k, v, o))
-    _check(lib().hyb_packed_attention(C.byref(desc), pq, pk, pv, po, cq, ck, ws, _nbytes(workspace), _stream()))
+    device, (pq, pk, pv, po, cq, ck) = _addresses((q, k, v, o, offsets_q, offsets_k), desc.like, _ATTENTION_NAMES)
+    ws, size = None, 0
+    if workspace is not None:
+        ws, size = _p(workspace), workspace.nbytes
+        if size and workspace.get_device() != device:
+            _here(workspace)
+    rc = lib().hyb_packed_attention(desc, pq, pk, pv, po, cq, ck, ws, size, torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc)
     return o
 
 

@@ -18,7 +18,7 @@ struct RotaryArgs {
     const int* positions;
     const void *q, *k;
     void *q_out, *k_out;
-    size_t q_stride, k_stride, q_out_stride, k_out_stride;   // elements
+    unsigned q_stride, k_stride, q_out_stride, k_out_stride;   // elements
     int tokens, axes;
     int head_dim, half;                 // half: pairs that turn
     int q_units, units;                 // units per token: of q, of q and k
@@ -51,25 +51,32 @@ __device__ __forceinline__ f32x2 cos_sin_turns(double t) {
     return f32x2{n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b};
 }
 
+// A kernel argument in a scalar register: a choice between two arguments is then one between values, not a load per lane from the chosen place.
+template <typename P> __device__ __forceinline__ P pinned(P x) {
+    asm("" : "+s"(x));
+    return x;
+}
+
 // A unit is what a thread turns at a time: HALVES: two 16-byte vectors half the rotated width apart (behind it two that are only scaled);
-// otherwise one vector of neighbouring pairs.
-template <typename T, bool HALVES>
+// otherwise one vector of neighbouring pairs.  FULL: all features of a head turn; then the queries' table holds the scale as well.
+template <typename T, bool HALVES, bool FULL>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     typedef typename Vec<T>::type vec;
-    constexpr int N = Vec<T>::n;
-    extern __shared__ f32x2 turn[];     // [tile][half]
+    constexpr int N = Vec<T>::n, PAIRS = HALVES ? N : N / 2;
+    extern __shared__ __attribute__((aligned(16))) f32x2 turn[];     // [tile][half] for k, and (FULL) the same times q_scale for q
     const int t0 = blockIdx.x * a.tile, tokens = min(a.tile, a.tokens - t0);
     const int total = tokens * a.units;
-    const T* in[kUnroll];
+    const T* q_in = pinned(static_cast<const T*>(a.q) + (size_t)t0 * a.q_stride);
+    const T* k_in = pinned(static_cast<const T*>(a.k) + (size_t)t0 * a.k_stride);
+    T* q_to = pinned(static_cast<T*>(a.q_out) + (size_t)t0 * a.q_out_stride);
+    T* k_to = pinned(static_cast<T*>(a.k_out) + (size_t)t0 * a.k_out_stride);
+    const unsigned q_step = pinned(a.q_stride), k_step = pinned(a.k_stride), q_to_step = pinned(a.q_out_stride), k_to_step = pinned(a.k_out_stride);
+    const int apart = a.half, apart_rest = a.head_dim / 2 - a.half;  // HALVES: elements between the two vectors of a unit that turns / does not
+    const int q_table = FULL ? tokens * a.half : 0;
     T* out[kUnroll];
     vec x[kUnroll], y[kUnroll];
-    int pair[kUnroll], token[kUnroll];
+    int pair[kUnroll], table[kUnroll];      // first pair (-1: no unit; FULL aside, >= half: does not turn); its place in `turn`
     float scale[kUnroll];
-    int apart = 0, apart_rest = 0;      // HALVES: elements between the two vectors
-    if constexpr (HALVES) {
-        apart = a.half;
-        apart_rest = a.head_dim / 2 - a.half;
-    }
     auto load = [&](int i0) {
 #pragma unroll
         for (int j = 0; j < kUnroll; j++) {
@@ -78,63 +85,69 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
             const int tok = quotient(i, a.unit_magic);
             int u = i - tok * a.units;
             const bool is_q = u < a.q_units;
-            const size_t at = t0 + tok;
-            const T* src = static_cast<const T*>(is_q ? a.q : a.k) + at * (is_q ? a.q_stride : a.k_stride);
-            T* dst = static_cast<T*>(is_q ? a.q_out : a.k_out) + at * (is_q ? a.q_out_stride : a.k_out_stride);
-            if (!is_q) u -= a.q_units;
-            scale[j] = is_q ? a.q_scale : 1.f;
-            token[j] = tok;
+            u -= is_q ? 0 : a.q_units;
             const int head = quotient(u, a.head_magic), v = u - head * a.head_units;
-            int off;
-            if constexpr (HALVES) {
-                const bool turned = v * N < a.half;
-                off = head * a.head_dim + (turned ? v * N : a.half + v * N);      // behind the rotated width R = 2 half: R + (v N - half)
-                pair[j] = turned ? v * N : kMaxPairs;
-            } else {
-                off = u * N;
-                pair[j] = v * (N / 2);
-            }
-            in[j] = src + off;
-            out[j] = dst + off;
-            x[j] = *reinterpret_cast<const vec*>(in[j]);
-            if constexpr (HALVES) y[j] = *reinterpret_cast<const vec*>(in[j] + (pair[j] < kMaxPairs ? apart : apart_rest));
+            scale[j] = is_q ? a.q_scale : 1.f;
+            pair[j] = v * PAIRS;
+            int off = u * N;
+            if constexpr (HALVES) off = head * a.head_dim + (FULL || pair[j] < a.half ? v * N : a.half + v * N);   // (behind the rotated width R = 2 half: R + (v N - half))
+            const T* in = (is_q ? q_in : k_in) + (size_t)(unsigned)tok * (is_q ? q_step : k_step) + off;
+            out[j] = (is_q ? q_to : k_to) + (size_t)(unsigned)tok * (is_q ? q_to_step : k_to_step) + off;
+            table[j] = (is_q ? q_table : 0) + tok * a.half + pair[j];
+            x[j] = *reinterpret_cast<const vec*>(in);
+            if constexpr (HALVES) y[j] = *reinterpret_cast<const vec*>(in + (FULL || pair[j] < a.half ? apart : apart_rest));
         }
     };
     auto finish = [&]() {
 #pragma unroll
         for (int j = 0; j < kUnroll; j++) {
             if (pair[j] < 0) continue;
-            const f32x2* cs = turn + token[j] * a.half;
-            vec u, w;
-            if constexpr (HALVES) {
-                const bool turned = pair[j] < kMaxPairs;
+            float p[PAIRS], q[PAIRS];
 #pragma unroll
-                for (int e = 0; e < N; e++) {
-                    const float p = to_f32<T>(x[j][e]) * scale[j], q = to_f32<T>(y[j][e]) * scale[j];
-                    const f32x2 c = cs[turned ? pair[j] + e : 0];
-                    u[e] = from_f32<T>(turned ? fmaf(p, c[0], -q * c[1]) : p);
-                    w[e] = from_f32<T>(turned ? fmaf(p, c[1], q * c[0]) : q);
-                }
-                *reinterpret_cast<vec*>(out[j]) = u;
-                *reinterpret_cast<vec*>(out[j] + (turned ? apart : apart_rest)) = w;
-            } else {
-#pragma unroll
-                for (int e = 0; e < N / 2; e++) {
-                    const float p = to_f32<T>(x[j][2 * e]) * scale[j], q = to_f32<T>(x[j][2 * e + 1]) * scale[j];
-                    const bool turned = pair[j] + e < a.half;
-                    const f32x2 c = cs[turned ? pair[j] + e : 0];
-                    u[2 * e] = from_f32<T>(turned ? fmaf(p, c[0], -q * c[1]) : p);
-                    u[2 * e + 1] = from_f32<T>(turned ? fmaf(p, c[1], q * c[0]) : q);
-                }
-                *reinterpret_cast<vec*>(out[j]) = u;
+            for (int e = 0; e < PAIRS; e++) {
+                p[e] = to_f32<T>(HALVES ? x[j][e] : x[j][2 * e]);
+                q[e] = to_f32<T>(HALVES ? y[j][e] : x[j][2 * e + 1]);
             }
+            if constexpr (!FULL) {
+#pragma unroll
+                for (int e = 0; e < PAIRS; e++) {
+                    p[e] *= scale[j];
+                    q[e] *= scale[j];
+                }
+            }
+            if (FULL || pair[j] < a.half) {
+                const f32x2* cs = turn + table[j];
+#pragma unroll
+                for (int e = 0; e < PAIRS; e++) {
+                    if (!FULL && !HALVES && pair[j] + e >= a.half) continue;       // (a vector may hold the last pairs that turn and the first that do not)
+                    const f32x2 c = cs[e];
+                    const float u = p[e];
+                    p[e] = fmaf(u, c[0], -q[e] * c[1]);
+                    q[e] = fmaf(u, c[1], q[e] * c[0]);
+                }
+            }
+            vec u, w;
+#pragma unroll
+            for (int e = 0; e < PAIRS; e++) {
+                if constexpr (HALVES) {
+                    u[e] = from_f32<T>(p[e]);
+                    w[e] = from_f32<T>(q[e]);
+                } else {
+                    u[2 * e] = from_f32<T>(p[e]);
+                    u[2 * e + 1] = from_f32<T>(q[e]);
+                }
+            }
+            *reinterpret_cast<vec*>(out[j]) = u;
+            if constexpr (HALVES) *reinterpret_cast<vec*>(out[j] + (FULL || pair[j] < a.half ? apart : apart_rest)) = w;
         }
     };
     load(threadIdx.x);                  // on their way while the angles are formed
     for (int i = threadIdx.x; i < tokens * a.half; i += kThreads) {
         const int tok = i / a.half, p = i - tok * a.half;
         const double pos = (double)a.positions[(size_t)(t0 + tok) * a.axes + a.axis[p]];
-        turn[i] = cos_sin_turns(pos * a.turns[p]);
+        const f32x2 c = cos_sin_turns(pos * a.turns[p]);
+        turn[i] = c;
+        if constexpr (FULL) turn[q_table + i] = f32x2{c[0] * a.q_scale, c[1] * a.q_scale};
     }
     __syncthreads();
     finish();
@@ -150,17 +163,29 @@ int launch(RotaryArgs& a, bool halves, int q_heads, int k_heads, hipStream_t st)
     a.head_units = a.head_dim / (halves ? 2 * N : N);
     a.q_units = q_heads * a.head_units;
     a.units = (q_heads + k_heads) * a.head_units;
-    // tokens per workgroup: about one round of loads, so that a long batch runs many workgroups and a short one still spreads over the chip
-    const int round = kThreads * kUnroll;
-    a.tile = a.units >= round ? 1 : round / a.units;
-    if (a.tile > 32) a.tile = 32;       // (32 x 128 pairs: 32 KB of LDS)
+    // Tokens per workgroup: of those that make two to four units per thread the number that leaves the fewest threads without one in the last round, the smaller for
+    // the same (32 / 8 heads of 128, 65537 tokens: 512 units 200 us, 1024 203, 2048 206; 256 units 399: workgroups are then not started fast enough.  24 heads of
+    // 64 have 384 units a token: two tokens 6.3 us, one 7.2 where fp32 has 12 and 12); and few tokens spread over the chip (16 tokens of 32 / 8 heads of 128: one 2.8 us,
+    // three 3.9).
+    a.tile = 1;
+    int best = 0;
+    for (int t = 1; t <= 16 && (t == 1 || (t * a.units <= 4 * kThreads && t * 400 <= a.tokens)); t++) {      // (16 x 128 pairs, twice: 32 KB of LDS)
+        const int n = t * a.units, share = 100 * n / ((n + kThreads - 1) / kThreads * kThreads);
+        if (share > best + 3 || (n > kThreads && (t - 1) * a.units <= kThreads)) {
+            a.tile = t;
+            best = share;
+        }
+    }
     a.unit_magic = magic_of((unsigned)a.units);
     a.head_magic = magic_of((unsigned)a.head_units);
+    const bool full = 2 * a.half == a.head_dim;
     const dim3 grid((unsigned)(((size_t)a.tokens + a.tile - 1) / a.tile));
-    const size_t lds = (size_t)a.tile * (a.half > 0 ? a.half : 1) * sizeof(f32x2);
+    const size_t lds = (size_t)a.tile * a.half * sizeof(f32x2) * (full ? 2 : 1);
     HybTraceScope trace("rotary", "byte", 2.0 * a.tokens * (q_heads + k_heads) * (double)a.head_dim * sizeof(T), st);
-    if (halves) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(kThreads), lds, st, a);
-    else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(kThreads), lds, st, a);
+    if (halves && full) hipLaunchKernelGGL((rotary_kernel<T, true, true>), grid, dim3(kThreads), lds, st, a);
+    else if (halves) hipLaunchKernelGGL((rotary_kernel<T, true, false>), grid, dim3(kThreads), lds, st, a);
+    else if (full) hipLaunchKernelGGL((rotary_kernel<T, false, true>), grid, dim3(kThreads), lds, st, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, false, false>), grid, dim3(kThreads), lds, st, a);
     return hyb_check_launch("rotary");
 }
 
@@ -203,7 +228,7 @@ extern "C" int hyb_rotary(const hyb_rotary_desc* desc, const int* positions, con
     RotaryArgs a = {};
     a.positions = positions;
     a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out;
-    a.q_stride = d.q_stride; a.k_stride = d.k_stride; a.q_out_stride = d.q_out_stride; a.k_out_stride = d.k_out_stride;
+    a.q_stride = (unsigned)d.q_stride; a.k_stride = (unsigned)d.k_stride; a.q_out_stride = (unsigned)d.q_out_stride; a.k_out_stride = (unsigned)d.k_out_stride;
     a.tokens = d.tokens; a.axes = d.axes; a.head_dim = d.head_dim; a.half = width / 2;
     a.q_scale = d.q_scale == 0.f ? 1.f : d.q_scale;
     // turns per position, theta^(-2 j / n) / (2 pi), by repeated multiplication in fp64: j roundings of 2^-53

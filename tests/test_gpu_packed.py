@@ -359,6 +359,47 @@ def test_attention_many_sequences(hb, dt):
     _check(dt, *_attention(hb, dt, lq, lk, 2, 1, 64, causal=True))
 
 
+@pytest.mark.parametrize("prescaled", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hq,hk,d", [(264, 264, 64), (260, 130, 128), (261, 261, 64), (272, 68, 128)])
+def test_attention_launches_of_many_rounds(hb, hq, hk, d, causal, prescaled):
+    """Thousands of row blocks, in several rounds of workgroups: the same bits as launches of a few heads; with scores far from zero in some heads, and with
+    infinities and NaN in keys that causal queries do not see."""
+    lq, lk = ([450, 77, 1, 0, 300, 5], [450, 77, 9, 4, 333, 0]) if d == 64 or not causal else ([600, 130, 1, 0, 700, 5], [600, 130, 9, 4, 733, 0])
+    g = torch.Generator(device="cuda").manual_seed(11)
+    q = torch.randn(sum(lq) + 4, hq, d, generator=g, device="cuda") * (d ** -0.5 * 1.4427 if prescaled else 1.0)
+    q[:, 3::16] *= 60.0
+    q = q.bfloat16()
+    k, v = (torch.randn(sum(lk) + 4, hk, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k[-4:] = float("nan")
+    v[-4:] = float("nan")
+    v[lk[0] - 2, :, 7] = float("inf")
+    cu_q, cu_k = _offsets(lq), _offsets(lk)
+    group = hq // hk
+
+    def run(h0, h1):
+        x = q[:, h0 * group:h1 * group], k[:, h0:h1], v[:, h0:h1], torch.full((len(q), (h1 - h0) * group, d), 7.0, device="cuda", dtype=torch.bfloat16)
+        desc = hb.packed_attention_desc(*x, cu_q, max(lq), max(lk), causal=causal, prescaled=prescaled)
+        ws = torch.full((hb.hyb_packed_attention_workspace_bytes(desc),), 255, device="cuda", dtype=torch.uint8)
+        for _ in range(3):
+            hb.hyb_packed_attention(desc, *x, cu_q, cu_k, ws)
+        return x[3]
+    whole = run(0, hk)
+    for h0 in range(0, hk, 10):
+        part = run(h0, min(h0 + 10, hk))
+        assert torch.equal(part.view(torch.int16), whole[:, h0 * group:min(h0 + 10, hk) * group].contiguous().view(torch.int16)), h0
+    assert (whole[sum(lq):] == 7.0).all()
+    last = [t for t in range(lq[0]) if not causal or t + lk[0] - lq[0] >= lk[0] - 2]
+    assert not torch.isfinite(whole[last[0]:lq[0], :, 7]).any() and torch.isfinite(whole[:last[0]]).all() and torch.isfinite(whole[lq[0]:]).all()
+    heads = [0, 3, group, hq - 1]
+    sub = lambda x, h: x[:, h].float().cpu().numpy().astype(np.float64)      # noqa: E731
+    rows = slice(lq[0], sum(lq))
+    for h in heads:
+        kk, vv = np.nan_to_num(sub(k, h // group)), np.nan_to_num(sub(v, h // group), posinf=0.0)
+        want = P.packed_attention(sub(q, h)[:, None], kk[:, None], vv[:, None], cu_q.tolist(), cu_k.tolist(), causal, 0.6931471805599453 if prescaled else d ** -0.5, np.full((len(q), 1, d), 7.0))
+        assert rel_l2(sub(whole, h)[rows], want[rows, 0]) < TOL_REL["bf16"], h
+
+
 def test_attention_a_request_does_not_depend_on_its_neighbours(hb):
     """The same sequence alone, in front and behind others, with the same sizes of the launch: the same bits."""
     q, k, v = (dev(synth.normal(s, (600, 4, 64), 1.0, "bf16"), torch.bfloat16) for s in (1, 2, 3))
