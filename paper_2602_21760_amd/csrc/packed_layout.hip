@@ -76,8 +76,10 @@ __device__ __forceinline__ Place place_of(int s, int4 sh, unsigned i, bool text_
 // Four rows per thread.  SCAN: every workgroup sums the lengths in LDS itself (requests <= kInOne), the first writes the offsets too: one launch;
 // otherwise the offsets are there.
 template <bool SCAN>
-__global__ __launch_bounds__(kThreads) void packed_rows_kernel(const int4* shapes, int requests, unsigned cap, int text_after, int* offsets, int* request, int* positions) {
+__global__ __launch_bounds__(kThreads) void packed_rows_kernel(const int4* shapes, int requests, unsigned cap, int text_after, int chunks, int* offsets, int* request, int* positions) {
     __shared__ unsigned own[SCAN ? kInOne + 1 : 1];
+    __shared__ int4 stage[kThreads / 64][192];
+    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     __shared__ unsigned wave_sums[kThreads / 64];
     if constexpr (SCAN) {
         unsigned carry = 0;
@@ -94,43 +96,72 @@ __global__ __launch_bounds__(kThreads) void packed_rows_kernel(const int4* shape
             for (int s = threadIdx.x; s <= requests; s += kThreads) offsets[s] = (int)own[s];
     }
     auto first_row = [&](int s) { return SCAN ? own[s] : (unsigned)offsets[s]; };
-    const unsigned r0 = ((unsigned)blockIdx.x * kThreads + threadIdx.x) * kRowsPerThread, rows = first_row(requests);
-    if (r0 >= rows) return;
-    int s = 0;                                      // the last request that begins at or before r0 and is not empty: first_row(s) <= r0 < first_row(s + 1)
-    for (int len = requests; len > 1;) {
-        const int half = len / 2;
-        if (first_row(s + half) <= r0) { s += half; len -= half; }
-        else len = half;
-    }
-    int4 sh = shapes[s];
-    unsigned begin = first_row(s), end = first_row(s + 1);
-    const int count = (int)min(rows - r0, (unsigned)kRowsPerThread);
-    int req[kRowsPerThread], pos[kRowsPerThread][3];
+    const unsigned rows = first_row(requests);
+    for (int chunk = 0; chunk < chunks; chunk++) {
+        const unsigned r0 = (((unsigned)blockIdx.x * chunks + chunk) * kThreads + threadIdx.x) * kRowsPerThread;
+        const unsigned wave0 = r0 - lane * kRowsPerThread;       // (the wave's first row)
+        if (r0 >= rows) return;
+        int s = 0;                                  // the last request that begins at or before r0: it is not empty, first_row(s) <= r0 < first_row(s + 1)
+        for (int len = requests; len > 1;) {
+            const int half = len / 2;
+            if (first_row(s + half) <= r0) { s += half; len -= half; }
+            else len = half;
+        }
+        int4 sh = shapes[s];
+        unsigned begin = first_row(s), end = first_row(s + 1);
+        int req[kRowsPerThread], pos[kRowsPerThread][3];
+        const unsigned i0 = r0 - begin;
+        const Place p = place_of(s, sh, i0, text_after != 0);
+        // four rows of one image (almost all threads): counting on from the first; otherwise row by row
+        const unsigned long long image = (unsigned long long)((unsigned)max(sh.y, 0) * (unsigned long long)max(sh.z, 0)) * (unsigned)max(sh.x, 0);
+        if (r0 + kRowsPerThread <= end && i0 + kRowsPerThread <= image) {
+            int t = p.t, y = p.y, x = p.x;
 #pragma unroll
-    for (int i = 0; i < kRowsPerThread; i++) {
-        if (i >= count) { req[i] = pos[i][0] = pos[i][1] = pos[i][2] = 0; continue; }
-        while (r0 + i >= end) {                     // (ends: r0 + i < rows = the end of the last request)
-            s++;
-            begin = end;
-            end = first_row(s + 1);
-            sh = shapes[s];
+            for (int i = 0; i < kRowsPerThread; i++) {
+                req[i] = s; pos[i][0] = t; pos[i][1] = y; pos[i][2] = x;
+                x++;
+                const int line = x == sh.z;
+                x = line ? 0 : x;
+                y += line;
+                const int frame = y == sh.y;
+                y = frame ? 0 : y;
+                t += frame;
+            }
+        } else {
+            const int count = (int)min(rows - r0, (unsigned)kRowsPerThread);
+#pragma unroll
+            for (int i = 0; i < kRowsPerThread; i++) {
+                if (i >= count) { req[i] = -1; pos[i][0] = pos[i][1] = pos[i][2] = 0; continue; }
+                while (r0 + i >= end) {             // (ends: r0 + i < rows = the end of the last request)
+                    s++;
+                    begin = end;
+                    end = first_row(s + 1);
+                    sh = shapes[s];
+                }
+                const Place p = place_of(s, sh, r0 + i - begin, text_after != 0);
+                req[i] = p.request; pos[i][0] = p.t; pos[i][1] = p.y; pos[i][2] = p.x;
+            }
         }
-        const Place p = place_of(s, sh, r0 + i - begin, text_after != 0);
-        req[i] = p.request; pos[i][0] = p.t; pos[i][1] = p.y; pos[i][2] = p.x;
-    }
-    if (count == kRowsPerThread) {
-        if (request) *reinterpret_cast<int4*>(request + r0) = make_int4(req[0], req[1], req[2], req[3]);
-        if (positions) {
-            int4* dst = reinterpret_cast<int4*>(positions + (size_t)r0 * 3);
-            dst[0] = make_int4(pos[0][0], pos[0][1], pos[0][2], pos[1][0]);
-            dst[1] = make_int4(pos[1][1], pos[1][2], pos[2][0], pos[2][1]);
-            dst[2] = make_int4(pos[2][2], pos[3][0], pos[3][1], pos[3][2]);
-        }
-    } else {
-        for (int i = 0; i < count; i++) {
-            if (request) request[r0 + i] = req[i];
-            if (positions)
-                for (int a = 0; a < 3; a++) positions[(size_t)(r0 + i) * 3 + a] = pos[i][a];
+        if (wave0 + 64 * kRowsPerThread <= rows) {
+            if (request) *reinterpret_cast<int4*>(request + r0) = make_int4(req[0], req[1], req[2], req[3]);
+            if (positions) {     // through LDS, so that a store of the wave writes 1 KB in a row and not every third 16 bytes of 3 KB
+                stage[wave][3 * lane] = make_int4(pos[0][0], pos[0][1], pos[0][2], pos[1][0]);
+                stage[wave][3 * lane + 1] = make_int4(pos[1][1], pos[1][2], pos[2][0], pos[2][1]);
+                stage[wave][3 * lane + 2] = make_int4(pos[2][2], pos[3][0], pos[3][1], pos[3][2]);
+                __builtin_amdgcn_wave_barrier();
+                int4* dst = reinterpret_cast<int4*>(positions + (size_t)wave0 * 3);
+#pragma unroll
+                for (int i = 0; i < 3; i++) dst[64 * i + lane] = stage[wave][64 * i + lane];
+                __builtin_amdgcn_wave_barrier();
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRowsPerThread; i++) {
+                if (req[i] < 0) continue;
+                if (request) request[r0 + i] = req[i];
+                if (positions)
+                    for (int a = 0; a < 3; a++) positions[(size_t)(r0 + i) * 3 + a] = pos[i][a];
+            }
         }
     }
 }
@@ -146,10 +177,12 @@ extern "C" int hyb_packed_layout(const int* shapes, int requests, int capacity, 
     const int4* sh = reinterpret_cast<const int4*>(shapes);
     const unsigned cap = (unsigned)capacity;
     const bool rows = requests > 0 && capacity > 0 && (request || positions);
-    const int groups = (int)(((size_t)capacity + kThreads * kRowsPerThread - 1) / (kThreads * kRowsPerThread));
+    // chunks of 1024 rows; workgroups take several in a row where there are more than the chip holds, so that the sums are made less often
+    const size_t all = ((size_t)capacity + kThreads * kRowsPerThread - 1) / (kThreads * kRowsPerThread), most = (size_t)hyb_cu_count() * 4;
+    const int chunks = requests <= kInOne ? (int)((all + most - 1) / most) : (all > 0), groups = chunks ? (int)((all + chunks - 1) / chunks) : 0;
     if (rows && requests <= kInOne) {
         HybTraceScope trace("packed_layout", "byte", 16.0 * requests + 16.0 * capacity, st);
-        hipLaunchKernelGGL(packed_rows_kernel<true>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, offsets, request, positions);
+        hipLaunchKernelGGL(packed_rows_kernel<true>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, chunks, offsets, request, positions);
         return hyb_check_launch("packed_layout");
     }
     {
@@ -159,6 +192,6 @@ extern "C" int hyb_packed_layout(const int* shapes, int requests, int capacity, 
     const int rc = hyb_check_launch("packed_offsets");
     if (rc != HYB_OK || !rows) return rc;
     HybTraceScope trace("packed_layout", "byte", 16.0 * capacity, st);
-    hipLaunchKernelGGL(packed_rows_kernel<false>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, offsets, request, positions);
+    hipLaunchKernelGGL(packed_rows_kernel<false>, dim3(groups), dim3(kThreads), 0, st, sh, requests, cap, text_after, chunks, offsets, request, positions);
     return hyb_check_launch("packed_layout");
 }
