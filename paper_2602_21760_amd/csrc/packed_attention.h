@@ -52,6 +52,7 @@ constexpr int kPackedRowsMfma = 128;                                            
 constexpr int kPackedRowsFew = 16;                                                   // bf16, few rows per sequence
 constexpr int kPackedRowsMerge = 4;                                                  // merge of cut keys: a wave per row
 constexpr int kPackedMaxParts = 64;                                                  // its lanes hold a part's weight each
+constexpr int packed_tile_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }    // keys of its LDS tiles
 constexpr int packed_rows_f32(int head_dim) { return head_dim == 64 ? 32 : 16; }     // fp32
 
 // Most blocks of `rows` rows that any offsets can ask for.

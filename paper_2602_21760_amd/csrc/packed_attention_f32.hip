@@ -255,7 +255,7 @@ int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
 }
 
 // How the keys are cut: `parts` workgroups per block of rows, the same number of keys each, where a launch's row blocks would leave most of the chip idle (the end of a long prompt).
-// max_k == 0: the keys of all sequences bound one sequence's.
+// max_k == 0: the keys of all sequences bound one sequence's.  slots: workgroups that the chip holds.
 void choose_parts(PackedAttnArgs& a, int max_k, int slots) {
     const long long units = (long long)a.blocks * a.k_heads;
     const int keys = max_k > 0 && max_k < a.total_k ? max_k : a.total_k;
@@ -312,13 +312,12 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     a.xcd_heads = d.k_heads % 8 == 0 ? 8 : d.k_heads % 4 == 0 ? 4 : d.k_heads % 2 == 0 ? 2 : 1;
     a.xcd_share = 8 / a.xcd_heads;
     a.parts = 1;
-    const int slots = hyb_cu_count() * (d.dtype == HYB_BF16 && d.head_dim == 64 ? 4 : 2);       // workgroups that the chip holds
     // at most 16 rows per sequence: the kernel whose waves split the keys (only the sizes that the caller names can say so; any others are right, too)
     if (d.dtype == HYB_BF16 && d.max_q > 0 && (long long)d.max_q * a.group <= kPackedRowsFew) {
-        choose_pieces(a, d.max_k, slots);
+        choose_pieces(a, d.max_k, hyb_cu_count() * (d.head_dim == 64 ? 4 : 2));
     } else {
         a.blocks = (int)packed_blocks(a, d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim));
-        choose_parts(a, d.max_k, slots);
+        choose_parts(a, d.max_k, hyb_cu_count() * (d.dtype == HYB_F32 ? 2 : d.head_dim == 64 ? 4 : 3));
     }
     return HYB_OK;
 }

@@ -1,7 +1,7 @@
-// Attention over packed batches for gfx950, bf16 operands, head_dim 64 or 128: a streaming softmax over 64-key tiles, scores never stored.
+// Attention over packed batches for gfx950, bf16 operands, head_dim 64 or 128: a streaming softmax over key tiles, scores never stored.
 //
 // A workgroup of 4 waves owns 128 rows (queries x heads of a group, see packed_attention.h) of one (sequence, key head), each wave 32 of
-// them (two tiles of 16).  Keys and values come 64 at a time through double-buffered LDS tiles by 16-byte direct-to-LDS copies, rows unpadded
+// them (two tiles of 16).  Keys and values come 64 (head_dim 128: 32) at a time through double-buffered LDS tiles of 8 KB by 16-byte direct-to-LDS copies, rows unpadded
 // with their 16-byte slots XOR-swizzled.  Both contractions run on v_mfma_f32_16x16x32_bf16 in transposed form, S^T = K Q^T and
 // O^T += V^T P^T: lane (l16 = lane % 16, q4 = lane / 16) of an accumulator tile holds column l16 and rows 4 q4 .. 4 q4 + 3, so all scores of a
 // lane belong to ONE row per 16-row tile, row sums are per-lane scalars plus two exchanges at the end, and the exponentiated scores of key tiles
@@ -16,6 +16,11 @@
 // "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA.  The first attempt lets them in; if a
 // result is not finite, the workgroup starts over in the same way as for sums out of range, and the second attempt searches every tile that not all rows see, zeroes such
 // values in the fragments and adds them to the rows that do see them.  (The search in the first attempt takes 3 to 9 % of launches over short sequences.)
+//
+// Bound by what the matrix cores sustain beside the softmax (16717 tokens, 24 heads of 64: 1170 TFLOP/s; 8192 tokens, 32 / 8 heads of 128: 1300, causal 1255) and, for short sequences, by the 5 us
+// that a workgroup takes before and after its key loop: 4 workgroups a CU at head_dim 64, 3 at 128.  (64 keys a tile at head_dim 128 take 200 registers, 2 workgroups a CU: 2 % slower on
+// 8192 tokens, 8 % on prompts of 33 to 4000, 14 % on prompts of 300.  Workgroups that walk through several units, the next one's first tile under way, from a queue filled by a
+// kernel before: as fast at head_dim 128, 20 % slower at 64.)
 #include "packed_attention.h"
 
 #include <type_traits>
@@ -23,7 +28,6 @@
 namespace {
 
 constexpr int BQ = kPackedRowsMfma;
-constexpr int BKV = 64;
 constexpr float RESCALE_LOG2 = 8.0f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -43,30 +47,27 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // Transposing LDS reads of the V^T fragments of 32 output features (two 16-feature tiles, two 32-key steps of two reads each).  Written as asm so that they can be issued
 // ahead of their use: a wait that the compiler places before such a read through its builtin also waits for the next tile's copies.  Every result goes
 // through lds_wait(), which stands between these reads and their use and keeps the registers in use until they are written.
-template <int D>
-__device__ __forceinline__ void v_reads(unsigned at, bf16x4 (&vh)[2][2][2]) {
+template <int D, int PS>
+__device__ __forceinline__ void v_reads(unsigned at, bf16x4 (&vh)[2][PS][2]) {
     constexpr int ROWB = D * 2;
 #pragma unroll
     for (int dd = 0; dd < 2; dd++)
 #pragma unroll
-        for (int ks = 0; ks < 2; ks++)
+        for (int ks = 0; ks < PS; ks++)
 #pragma unroll
             for (int half = 0; half < 2; half++)
                 asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(vh[dd][ks][half]) : "v"(dd ? at ^ 32u : at), "i"((ks * 32 + half * 16) * ROWB));
 }
 // Waits until at most YOUNGER LDS reads are outstanding; reads complete in order.
 template <int YOUNGER>
-__device__ __forceinline__ void lds_wait(bf16x4 (&vh)[2][2][2], bf16x8 (&vf)[2][2]) {
+__device__ __forceinline__ void lds_wait(bf16x4 (&vh)[2][2][2]) {
     asm volatile("s_waitcnt lgkmcnt(%8)"
                  : "+v"(vh[0][0][0]), "+v"(vh[0][0][1]), "+v"(vh[0][1][0]), "+v"(vh[0][1][1]), "+v"(vh[1][0][0]), "+v"(vh[1][0][1]), "+v"(vh[1][1][0]), "+v"(vh[1][1][1])
                  : "n"(YOUNGER));
-#pragma unroll
-    for (int dd = 0; dd < 2; dd++)
-#pragma unroll
-        for (int ks = 0; ks < 2; ks++) {
-            const bf16x4 lo = vh[dd][ks][0], hi = vh[dd][ks][1];
-            vf[dd][ks] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        }
+}
+template <int YOUNGER>
+__device__ __forceinline__ void lds_wait(bf16x4 (&vh)[2][1][2]) {
+    asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(vh[0][0][0]), "+v"(vh[0][0][1]), "+v"(vh[1][0][0]), "+v"(vh[1][0][1]) : "n"(YOUNGER));
 }
 
 // The same for a K fragment: requested, and awaited with at most YOUNGER reads outstanding.
@@ -84,6 +85,13 @@ __device__ __forceinline__ void unrolled(F f) {
     }
 }
 
+// Everything that makes these values stands before, everything that uses them behind this place.
+template <typename V, int N>
+__device__ __forceinline__ void keep_order(V (&x)[N][2]) {
+#pragma unroll
+    for (int i = 0; i < N; i++) asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]));
+}
+
 // The lane's index from an instruction the compiler cannot trace back: what rare paths and the epilogue derive from it is not kept in registers over the key loop.
 __device__ __forceinline__ int lane_again() {
     int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -92,7 +100,8 @@ __device__ __forceinline__ int lane_again() {
 }
 
 template <int D, bool PRE>
-__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(PackedAttnArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(PackedAttnArgs a) {
+    constexpr int BKV = packed_tile_keys(D), KT = BKV / 16, PS = BKV / 32;      // keys of a tile; 16-key tiles; 32-key steps of the second contraction
     constexpr int ROWB = D * 2, TILE_BYTES = BKV * ROWB, SLOTS = ROWB / 16;
     constexpr int CHUNK_ROWS = 1024 / ROWB, CHUNKS = BKV / CHUNK_ROWS / 4;      // rows of a 1 KB copy; copies per wave, operand and tile
     constexpr int KS = D / 32, DT = D / 16, VG = D / 32;
@@ -189,25 +198,25 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
         if (PLAIN ? !active : t * BKV > wave_max) return;  // none of the wave's rows sees this tile
         const bool masked = !PLAIN && t * BKV + BKV - 1 > wave_min;
 
-        // S^T = K Q^T; the K fragments (step j / 4, key tile j % 4) flow through a ring of four reads that run ahead of the MFMAs
+        // S^T = K Q^T; the K fragments (step j / KT, key tile j % KT) flow through a ring of four reads that run ahead of the MFMAs
         bf16x8 ring[4];
         __builtin_amdgcn_s_setprio(1);
-        auto k_frag = [&](auto j) { k_read<(j.value & 3) * 16 * ROWB>(kb ^ ((j.value >> 2) * 64u), ring[j.value & 3]); };
+        auto k_frag = [&](auto j) { k_read<(j.value % KT) * 16 * ROWB>(kb ^ ((j.value / KT) * 64u), ring[j.value & 3]); };
         unrolled<4>(k_frag);
-        f32x4 s[4][2];   // [key tile][row tile]: keys 16 kt + 4 q4 .. + 3 of row 16 qt + l16
+        f32x4 s[KT][2];   // [key tile][row tile]: keys 16 kt + 4 q4 .. + 3 of row 16 qt + l16
 #pragma unroll
-        for (int kt = 0; kt < 4; kt++)
+        for (int kt = 0; kt < KT; kt++)
 #pragma unroll
             for (int qt = 0; qt < 2; qt++) s[kt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        unrolled<4 * KS>([&](auto j) {
+        unrolled<KT * KS>([&](auto j) {
             constexpr int J = j.value;
-            k_wait<(4 * KS - 1 - J < 3 ? 4 * KS - 1 - J : 3)>(ring[J & 3]);
+            k_wait<(KT * KS - 1 - J < 3 ? KT * KS - 1 - J : 3)>(ring[J & 3]);
 #pragma unroll
-            for (int qt = 0; qt < 2; qt++) s[J & 3][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[J & 3], qf[qt][J >> 2], s[J & 3][qt], 0, 0, 0);
-            if constexpr (J + 4 < 4 * KS) k_frag(std::integral_constant<int, J + 4>{});
+            for (int qt = 0; qt < 2; qt++) s[J % KT][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[J & 3], qf[qt][J / KT], s[J % KT][qt], 0, 0, 0);
+            if constexpr (J + 4 < KT * KS) k_frag(std::integral_constant<int, J + 4>{});
         });
 
-        bf16x4 vh[2][2][2][2];   // [two groups of 32 features in flight][16-feature tile][32-key step][read]
+        bf16x4 vh[2][2][PS][2];   // [two groups of 32 features in flight][16-feature tile][32-key step][read]
         bool odd = false;        // infinities or NaN among the values of a tile that not all rows see (looked for in the second attempt only)
         if (masked) {
             const int ln = lane_again();
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             for (int qt = 0; qt < 2; qt++) {
                 const int seen = row_last[wave * 32 + qt * 16 + ln % 16] - t * BKV - 4 * (ln / 16);     // keys 16 kt + i > seen are hidden
 #pragma unroll
-                for (int kt = 0; kt < 4; kt++)
+                for (int kt = 0; kt < KT; kt++)
 #pragma unroll
                     for (int i = 0; i < 4; i++)
                         if (kt * 16 + i > seen) s[kt][qt][i] = -__builtin_inff();
@@ -231,28 +240,28 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
                 odd = __any(any != 0);
             }
         }
-        if constexpr (DIRECT) v_reads<D>(vb, vh[0]);       // (the form with row maxima holds more values meanwhile and requests them after them)
+        if constexpr (DIRECT) v_reads<D, PS>(vb, vh[0]);       // (the form with row maxima holds more values meanwhile and requests them after them)
         // the exponentiated scores of key tiles 2 ks, 2 ks + 1, rounded to bf16, are the B operand of 32-key step ks
         if constexpr (DIRECT && !PRE) {
 #pragma unroll
-            for (int kt = 0; kt < 4; kt++)
+            for (int kt = 0; kt < KT; kt++)
 #pragma unroll
                 for (int qt = 0; qt < 2; qt++) s[kt][qt] *= c;
-            asm volatile("" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]), "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
+            keep_order(s);
         }
         __builtin_amdgcn_s_setprio(0);     // a wave yields during its exponentials, so that they do not hold up another wave's MFMAs
-        bf16x8 pb[2][2];   // [32-key step][row tile]
+        bf16x8 pb[PS][2];   // [32-key step][row tile]
         if constexpr (DIRECT) {
 #pragma unroll
-            for (int kt = 0; kt < 4; kt++)
+            for (int kt = 0; kt < KT; kt++)
 #pragma unroll
                 for (int qt = 0; qt < 2; qt++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) s[kt][qt][i] = __builtin_amdgcn_exp2f(s[kt][qt][i]);
-            asm volatile("" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]), "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
+            keep_order(s);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int kt = 0; kt < 4; kt++)
+            for (int kt = 0; kt < KT; kt++)
 #pragma unroll
                 for (int qt = 0; qt < 2; qt++)
 #pragma unroll
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             for (int qt = 0; qt < 2; qt++) {
                 float m0 = s[0][qt][0];
 #pragma unroll
-                for (int kt = 0; kt < 4; kt++) m0 = max3(max3(s[kt][qt][0], s[kt][qt][1], m0), s[kt][qt][2], s[kt][qt][3]);
+                for (int kt = 0; kt < KT; kt++) m0 = max3(max3(s[kt][qt][0], s[kt][qt][1], m0), s[kt][qt][2], s[kt][qt][3]);
                 m0 = max3(m0, __shfl_xor(m0, 16, 64), m0);
                 mx[qt] = max3(m0, __shfl_xor(m0, 32, 64), m0);
             }
@@ -284,46 +293,46 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_kernel(
             for (int qt = 0; qt < 2; qt++) {
                 const float mc = m_run[qt] == -__builtin_inff() ? 0.f : m_run[qt] * c;
 #pragma unroll
-                for (int kt = 0; kt < 4; kt++)
+                for (int kt = 0; kt < KT; kt++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[kt][qt][i], c, -mc));
             }
-            asm volatile("" : "+v"(pb[0][0]), "+v"(pb[0][1]), "+v"(pb[1][0]), "+v"(pb[1][1]));
+            keep_order(pb);
             __builtin_amdgcn_s_setprio(1);
-            v_reads<D>(vb, vh[0]);
+            v_reads<D, PS>(vb, vh[0]);
         }
 
         // O^T += V^T P^T, 32 features at a time, the next 32 on their way
 #pragma unroll
         for (int g = 0; g < VG; g++) {
-            bf16x8 vf[2][2];
             if (g + 1 < VG) {
-                v_reads<D>(vb ^ ((g + 1) * 64u), vh[(g + 1) & 1]);
-                lds_wait<8>(vh[g & 1], vf);
+                v_reads<D, PS>(vb ^ ((g + 1) * 64u), vh[(g + 1) & 1]);
+                lds_wait<4 * PS>(vh[g & 1]);
             } else {
-                lds_wait<0>(vh[g & 1], vf);
+                lds_wait<0>(vh[g & 1]);
             }
             if (!DIRECT && odd) {
 #pragma unroll
                 for (int dd = 0; dd < 2; dd++)
 #pragma unroll
-                    for (int ks = 0; ks < 2; ks++) {
-                        u32x4 w = __builtin_bit_cast(u32x4, vf[dd][ks]);
-#pragma unroll
-                        for (int e = 0; e < 4; e++) w[e] &= ~odd_mask_bf16(w[e]);
-                        vf[dd][ks] = __builtin_bit_cast(bf16x8, w);
+                    for (int ks = 0; ks < PS; ks++) {
+                        keep_finite(vh[g & 1][dd][ks][0]);
+                        keep_finite(vh[g & 1][dd][ks][1]);
                     }
             }
 #pragma unroll
             for (int dd = 0; dd < 2; dd++)
 #pragma unroll
-                for (int ks = 0; ks < 2; ks++)
+                for (int ks = 0; ks < PS; ks++) {
+                    const bf16x4 lo = vh[g & 1][dd][ks][0], hi = vh[g & 1][dd][ks][1];
+                    const bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
-                    for (int qt = 0; qt < 2; qt++) o[2 * g + dd][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dd][ks], pb[ks][qt], o[2 * g + dd][qt], 0, 0, 0);
+                    for (int qt = 0; qt < 2; qt++) o[2 * g + dd][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[ks][qt], o[2 * g + dd][qt], 0, 0, 0);
+                }
             if (g == 0) {        // the normaliser, from the rounded probabilities, beside the MFMAs
                 const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
 #pragma unroll
-                for (int ks = 0; ks < 2; ks++)
+                for (int ks = 0; ks < PS; ks++)
 #pragma unroll
                     for (int qt = 0; qt < 2; qt++)
 #pragma unroll
