@@ -29,9 +29,8 @@ struct PackedAttnArgs {
     int causal, prescaled;
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
     int blocks;                                   // row blocks of all sequences, an upper bound (see find_block)
-    int parts, part_keys;                         // keys are cut into `parts` of part_keys keys (the last part takes what is left); 1: not cut
-                                                  // (few-rows kernel: 1, and pieces of part_keys keys)
-    int pieces;                                   // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
+    int parts;                                    // the keys of a block are cut into up to `parts` parts (see packed_part_tiles); 1: not cut
+    int pieces, part_keys;                        // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
     float* part;                                  // scratch (see below)
     int xcd_heads, xcd_share;                     // gcd(8, k_heads), 8 / gcd
 };
@@ -52,6 +51,7 @@ constexpr int kPackedRowsMfma = 128;                                            
 constexpr int kPackedRowsFew = 16;                                                   // bf16, few rows per sequence
 constexpr int kPackedRowsMerge = 4;                                                  // merge of cut keys: a wave per row
 constexpr int kPackedMaxParts = 64;                                                  // its lanes hold a part's weight each
+constexpr int kPackedPartKeys = 256;                                                 // least keys of a part
 constexpr int packed_tile_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }    // keys of its LDS tiles
 constexpr int packed_rows_f32(int head_dim) { return head_dim == 64 ? 32 : 16; }     // fp32
 
@@ -166,6 +166,11 @@ __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a, unsig
     u.rows = (int)max(min(all - row0, (long long)ROWS), 0ll);
     u.row0 = (int)row0;           // (meaningful when rows > 0: below total_q * group, which the launcher keeps below 2^31)
     return u;
+}
+
+// Tiles of a part of a block that sees nt tiles of `tile` keys: even shares, which need no knowledge of the longest sequence on the host.
+__device__ __forceinline__ int packed_part_tiles(const PackedAttnArgs& a, int nt, int tile) {
+    return a.parts == 1 ? nt : max((nt + a.parts - 1) / a.parts, kPackedPartKeys / tile);
 }
 
 // Last key that query t of a sequence sees (-1: none).

@@ -42,9 +42,8 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
         for (int s = 0; s < DT; s++) q[qt][s] = *reinterpret_cast<const f32x4*>(qp + 64 * s + 16 * q4);
     }
     const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group)), block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
-    const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;
-    const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
-    const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
+    const int nt = (block_max + BKV) / BKV, part_tiles = packed_part_tiles(a, nt, BKV);
+    const int t_begin = min(u.part * part_tiles, nt), t_end = min(t_begin + part_tiles, nt);
 
     float m[QT], l[QT];
     f32x4 o[DT][QT];     // [feature tile][row tile]
@@ -254,7 +253,7 @@ int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
     return hyb_check_launch("packed_attention_merge");
 }
 
-// How the keys are cut: `parts` workgroups per block of rows, the same number of keys each, where a launch's row blocks would leave most of the chip idle (the end of a long prompt).
+// How the keys are cut: `parts` workgroups per block of rows where a launch's row blocks would leave most of the chip idle (the end of a long prompt); each block deals its own keys out to them.
 // max_k == 0: the keys of all sequences bound one sequence's.  slots: workgroups that the chip holds.
 void choose_parts(PackedAttnArgs& a, int max_k, int slots) {
     const long long units = (long long)a.blocks * a.k_heads;
@@ -262,20 +261,20 @@ void choose_parts(PackedAttnArgs& a, int max_k, int slots) {
     if (units == 0 || units * 2 > slots || keys <= 512) return;
     long long parts = slots / units;
     if (parts > kPackedMaxParts) parts = kPackedMaxParts;
-    long long len = ((keys + parts - 1) / parts + 63) / 64 * 64;
-    if (len < 256) len = 256;
-    if (len >= keys) return;
-    a.parts = (int)((keys + len - 1) / len);
-    a.part_keys = (int)len;
+    const long long most = (keys + kPackedPartKeys - 1) / kPackedPartKeys;
+    a.parts = (int)(parts < most ? parts : most);
 }
 // Pieces of the few-rows kernel: all keys dealt out over the chip, two pieces for every workgroup that fits it (one: 11 % slower over caches of 100 to 8000 keys, three: the same), of at
 // least 256 keys (8000 keys of one sequence, 8 heads of 128: 11.7 us; of 512: 13.0), or 512 where the sequences alone fill the chip.  Sequences of which the caller says that none is
-// longer than a piece are one piece each, whatever their length, and need no join.
+// longer than a piece are one piece each, whatever their length, and need no join.  So are those of up to 2048 keys and much the same length that keep a third of the chip busy: what
+// pieces cost in starts and join is more than what they even out (8 heads of 128: 40 caches of 630 to 700 keys 24.8 us, in pieces 31.0; 87 of 1080 to 1200 77 / 97; 53 of 1800 to 2000
+// 82 / 93; of 2700 to 3000 125 / 132, but 40 of them 110 / 103.  256 caches of which every second has 2000 keys, the others 50, 4 heads: 130 / 118).
 void choose_pieces(PackedAttnArgs& a, int max_k, int slots) {
     long long len = ((long long)a.total_k * a.k_heads / (2 * slots) + 63) / 64 * 64;
     const int least = (long long)a.sequences * a.k_heads >= slots ? 512 : 256;
     if (len < least) len = least;
-    if (max_k > 0 && max_k <= len) len = 1 << 30;
+    const bool alike = max_k <= 2048 && 4ll * a.sequences * max_k <= 7ll * a.total_k && 3ll * a.total_k * a.k_heads >= (long long)max_k * slots;
+    if (max_k > 0 && (max_k <= len || alike)) len = 1 << 30;
     a.part_keys = (int)len;
     a.pieces = (int)(a.total_k / len) + a.sequences;
     a.blocks = (int)packed_blocks(a, 1);       // of the join

@@ -135,9 +135,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
     const int wave_max = active ? packed_last_key(a, u, packed_div(u.row0 + min(wave * 32 + 31, u.rows - 1), a.by_group)) : -1;
     const int block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
 
-    const int part_tiles = a.part_keys / BKV, nt = (block_max + BKV) / BKV;                    // (block_max == -1: no tile)
-    const int t_begin = a.parts > 1 ? min(u.part * part_tiles, nt) : 0;
-    const int t_end = a.parts > 1 && u.part < a.parts - 1 ? min(t_begin + part_tiles, nt) : nt;
+    const int nt = (block_max + BKV) / BKV, part_tiles = packed_part_tiles(a, nt, BKV);        // (block_max == -1: no tile)
+    const int t_begin = min(u.part * part_tiles, nt), t_end = min(t_begin + part_tiles, nt);
     // Tiles t_begin .. plain_end - 1 are seen whole by all rows and followed by a tile of 64 keys: a loop of its own, which holds no masks in registers.
     const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group));
     const int plain_end = min(min((block_min + 1) / BKV, u.n_k / BKV - 1), t_end - 1);

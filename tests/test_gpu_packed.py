@@ -240,6 +240,25 @@ def test_attention_few_queries_over_long_keys(hb, dt, case, causal):
     _check(dt, *got)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_many_caches_of_much_the_same_length(hb, dt):
+    """Single tokens whose caches alone fill the chip: not cut."""
+    for hq, hk, d in ((16, 8, 64), (8, 8, 128)):
+        *got, need = _attention(hb, dt, [1] * 60, [600 - 3 * i for i in range(60)], hq, hk, d, causal=True)
+        assert need == 0
+        _check(dt, *got)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_cut_keys_without_hints(hb, dt, d):
+    """One long cache among short and empty ones: every block deals its own keys out, down to parts of 256."""
+    lq, lk = [1, 3, 1, 0, 2, 1, 1, 1, 4], [3000, 40, 0, 9, 700, 257, 256, 255, 513]
+    *got, need = _attention(hb, dt, lq, lk, 4, 2, d, causal=True, hints=False)
+    assert need > 0
+    _check(dt, *got)
+
+
 @pytest.mark.parametrize("hints", [False, 1, 600, 100000])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_hints_do_not_decide_the_result(hb, dt, hints):
