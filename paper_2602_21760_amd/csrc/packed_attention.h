@@ -31,6 +31,7 @@ struct PackedAttnArgs {
     int blocks;                                   // row blocks of all sequences, an upper bound (see find_block)
     int parts;                                    // the keys of a block are cut into up to `parts` parts (see packed_part_tiles); 1: not cut
     int pieces, part_keys;                        // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
+    int rests_last;                               // few-rows kernel: pieces that are not full come last (see piece_in_order)
     float* part;                                  // scratch (see below)
     int xcd_heads, xcd_share;                     // gcd(8, k_heads), 8 / gcd
 };

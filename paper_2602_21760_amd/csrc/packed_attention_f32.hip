@@ -277,6 +277,7 @@ void choose_pieces(PackedAttnArgs& a, int max_k, int slots) {
     if (max_k > 0 && (max_k <= len || alike)) len = 1 << 30;
     a.part_keys = (int)len;
     a.pieces = (int)(a.total_k / len) + a.sequences;
+    a.rests_last = a.sequences <= 64 && (long long)a.pieces * a.k_heads > slots;
     a.blocks = (int)packed_blocks(a, 1);       // of the join
 }
 

@@ -249,6 +249,18 @@ def test_attention_many_caches_of_much_the_same_length(hb, dt):
         _check(dt, *got)
 
 
+@pytest.mark.parametrize("sequences", [40, 64, 65])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_many_ragged_caches(hb, d, sequences):
+    """Several rounds of pieces: full ones, rests of all sizes, none at all and empty caches; two queries here and there, or none."""
+    lk = [(3100, 0, 256, 512, 700, 1, 255, 257, 1024, 60)[i % 10] + i // 10 * (i % 3) for i in range(sequences)]
+    lq = [(1, 1, 2, 1, 0, 1, 2)[i % 7] for i in range(sequences)]
+    for causal in (False, True):
+        *got, need = _attention(hb, "bf16", lq, lk, 16, 16 if d == 64 else 8, d, causal=causal)
+        assert need > 0
+        _check("bf16", *got)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_cut_keys_without_hints(hb, dt, d):
