@@ -1,23 +1,24 @@
 // fp32 attention over packed batches on the fp32 matrix cores (reference precision), the merge of cut keys for both types, and the entry point.
 //
 // As attention_f32.hip: a workgroup of 4 waves owns 32 rows (head_dim 128: 16) of one (sequence, key head) and splits the KEYS: wave w takes the 32-key
-// tiles w, w + 4, ... with a running maximum and normaliser of its own; the four partial results are merged in LDS in a fixed order.  Operands go
+// tiles w, w + 4, ... with a running reference and normaliser of its own; the four partial results are merged in LDS in a fixed order.  Operands go
 // straight from memory (L2) to registers.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: a 16-byte load gives a lane 4 features of its key
 // for 4 MFMAs, and register i of the exponentiated S^T is the B operand of the MFMA over the keys 4 q4 + i, with rows 4 q4 + i of V as the A operand.
+//
+// Bound by the matrix cores, which share their issue with everything else here: fp32 MFMAs and vector instructions of the two waves of a SIMD do not overlap (busy 63 % and 24 % of the time
+// with 382 vector instructions beside the 128 MFMAs of a tile, no better with waves of different priority).  So a tile has few others: a probability is one fma and one
+// v_exp_f32, 2^(c score - reference), whose error is that of an argument near 0 wherever the probability counts; masks, maxima across lanes and rescaling only where a tile asks for them;
+// offsets of buffer loads that no tile changes.  One sequence of 4096, 8 heads: head_dim 64 127 TFLOP/s, 128 107 (a large library product in fp32 reaches 139); 16 rows at head_dim 64 110.
+// Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles and by the last round (314, 1302 and 259 tokens, 12 / 4 heads of 64: 65 us, 88 TFLOP/s).
 #include "packed_attention.h"
 
 namespace {
 
 constexpr int BKV = 32;
 constexpr int WAVES = 4;
+constexpr float RESCALE_LOG2 = 8.0f;
 
-// e^x for x <= 0 to 1.5 ulp: 2^n 2^f with n = x log2(e) rounded and f the rest, log2(e) in two parts; NaN stays NaN.
-__device__ __forceinline__ float exp_neg(float x) {
-    x = x < -200.f ? -200.f : x;
-    const float n = rintf(x * 1.44269502162933349609375f);
-    const float f = fmaf(x, 1.92596299112661746887e-8f, fmaf(x, 1.44269502162933349609375f, -n));
-    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
-}
+__device__ __forceinline__ f32x4 load16(__amdgpu_buffer_rsrc_t rsrc, int offset) { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0)); }
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
@@ -31,6 +32,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
     const char* kp = static_cast<const char*>(a.k) + (size_t)u.k0 * a.k_token + (size_t)u.head * a.k_head;
     const char* vp = static_cast<const char*>(a.v) + (size_t)u.k0 * a.v_token + (size_t)u.head * a.v_head;
 
+    const float c = a.prescaled ? 1.f : a.scale * 1.4426950408889634f;
     f32x4 q[QT][DT];     // [row tile][16-feature step]
     int last[QT];
 #pragma unroll
@@ -54,23 +56,37 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) o[dt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int t = t_begin + wave; t < t_end; t += WAVES) {
-        const int key0 = t * BKV;
-        f32x4 k[2][DT], v[2][4][VH];     // K: [key tile][16-feature step]; V: [key tile][row 4 q4 + i][64 features]
+    // byte offsets of the lane's rows in a tile; rows behind the last key lie outside the resource and come as zeros
+    int k_off[2], v_off[2][4];
 #pragma unroll
-        for (int kt = 0; kt < 2; kt++) {
-            const char* row = kp + (size_t)min(key0 + kt * 16 + l16, u.n_k - 1) * a.k_token + 16 * q4;
+    for (int kt = 0; kt < 2; kt++) {
+        k_off[kt] = (kt * 16 + l16) * (int)a.k_token + 16 * q4;
 #pragma unroll
-            for (int s = 0; s < DT; s++) k[kt][s] = *reinterpret_cast<const f32x4*>(row + 64 * s);
-        }
+        for (int i = 0; i < 4; i++) v_off[kt][i] = (kt * 16 + 4 * q4 + i) * (int)a.v_token + 16 * l16;
+    }
+    f32x4 k[2][DT];      // [key tile][16-feature step]
+    auto load_k = [&](int t) {
+        const int key0 = t * BKV, more = min(u.n_k - key0, BKV) - 1;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)key0 * a.k_token), 0, more * (int)a.k_token + 4 * D, 0x00020000);
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const char* row = vp + (size_t)min(key0 + kt * 16 + 4 * q4 + i, u.n_k - 1) * a.v_token + 16 * l16;
+            for (int s = 0; s < DT; s++) k[kt][s] = load16(rsrc, k_off[kt] + 64 * s);
+    };
+    // head_dim 64: the next tile's keys are requested as soon as this one's scores stand (one sequence of 4096, 8 heads: 277 us without, 271 so; at 128 it takes registers that are not there)
+    constexpr bool AHEAD = D == 64;
+    if (AHEAD && t_begin + wave < t_end) load_k(t_begin + wave);
+    for (int t = t_begin + wave; t < t_end; t += WAVES) {
+        const int key0 = t * BKV, more = min(u.n_k - key0, BKV) - 1;
+        const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + (size_t)key0 * a.v_token), 0, more * (int)a.v_token + 4 * D, 0x00020000);
+        f32x4 v[2][4][VH];   // [key tile][row 4 q4 + i][64 features]
+        if constexpr (!AHEAD) load_k(t);
 #pragma unroll
-                for (int h = 0; h < VH; h++) v[kt][i][h] = *reinterpret_cast<const f32x4*>(row + 256 * h);
-            }
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int h = 0; h < VH; h++) v[kt][i][h] = load16(v_rsrc, v_off[kt][i] + 256 * h);
         f32x4 s[2][QT];      // [key tile][row tile]: keys 16 kt + 4 q4 + i
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
@@ -84,30 +100,47 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
                 for (int kt = 0; kt < 2; kt++)
 #pragma unroll
                     for (int qt = 0; qt < QT; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][st][j], q[qt][st][j], s[kt][qt], 0, 0, 0);
+        if constexpr (AHEAD) load_k(min(t + WAVES, t_end - 1));      // (the last one again: with a branch, the wait for the values would be one for these)
         const bool masked = key0 + BKV - 1 > block_min;
+        if (masked) {
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) {
+                const int seen = last[qt] - key0 - 4 * q4;      // keys 16 kt + i > seen are hidden
+#pragma unroll
+                for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) s[kt][qt][i] = kt * 16 + i > seen ? -__builtin_inff() : s[kt][qt][i];
+            }
+        }
+        // the reference m (in base 2) only advances when a score exceeds it by more than 2^RESCALE_LOG2; it is the same for the four lanes of a row
+        float mx[QT];
+        bool grows = false;
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
-            const int seen = last[qt] - key0 - 4 * q4;      // keys 16 kt + i > seen are hidden
+            mx[qt] = fmaxf(fmaxf(fmaxf(s[0][qt][0], s[0][qt][1]), fmaxf(s[0][qt][2], s[0][qt][3])), fmaxf(fmaxf(s[1][qt][0], s[1][qt][1]), fmaxf(s[1][qt][2], s[1][qt][3])));
+            grows |= fmaf(mx[qt], c, -m[qt]) > RESCALE_LOG2;
+        }
+        if (__any(grows)) {
 #pragma unroll
-            for (int kt = 0; kt < 2; kt++)
+            for (int qt = 0; qt < QT; qt++) {
+                mx[qt] = fmaxf(mx[qt], __shfl_xor(mx[qt], 16, 64));
+                mx[qt] = fmaxf(mx[qt], __shfl_xor(mx[qt], 32, 64)) * c;
+                const bool grow = mx[qt] - m[qt] > RESCALE_LOG2;
+                const float corr = grow ? __builtin_amdgcn_exp2f(m[qt] - mx[qt]) : 1.f;      // first tile: 2^-inf = 0
+                m[qt] = grow ? mx[qt] : m[qt];
+                l[qt] *= corr;
 #pragma unroll
-                for (int i = 0; i < 4; i++) s[kt][qt][i] = kt * 16 + i > seen ? -__builtin_inff() : s[kt][qt][i] * a.scale;
-            float mx = fmaxf(fmaxf(fmaxf(s[0][qt][0], s[0][qt][1]), fmaxf(s[0][qt][2], s[0][qt][3])),
-                             fmaxf(fmaxf(s[1][qt][0], s[1][qt][1]), fmaxf(s[1][qt][2], s[1][qt][3])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m[qt], mx);
-            const float corr = m[qt] == m_new ? 1.f : exp_neg(m[qt] - m_new);   // first tile: exp(-inf) = 0
-            m[qt] = m_new;
-            l[qt] *= corr;
+                for (int dt = 0; dt < DT; dt++) o[dt][qt] *= corr;
+            }
+        }
 #pragma unroll
-            for (int dt = 0; dt < DT; dt++) o[dt][qt] *= corr;
-            const float ref = m_new == -__builtin_inff() ? 0.f : m_new;          // only hidden keys so far: all probabilities 0
+        for (int qt = 0; qt < QT; qt++) {
+            const float ref = m[qt] == -__builtin_inff() ? 0.f : m[qt];          // only hidden keys so far: all probabilities 0
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    s[kt][qt][i] = exp_neg(s[kt][qt][i] - ref);
+                    s[kt][qt][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][qt][i], c, -ref));
                     l[qt] += s[kt][qt][i];
                 }
         }
@@ -155,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
                     for (int qt = 0; qt < QT; qt++) o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[kt][i][dt / 4][dt % 4], s[kt][qt][i], o[dt][qt], 0, 0, 0);
     }
 
-    // merge of the waves: row = sum_p o_p e^(m_p - M) / sum_p l_p e^(m_p - M), p in order
+    // merge of the waves: row = sum_p o_p 2^(m_p - M) / sum_p l_p 2^(m_p - M), p in order
 #pragma unroll
     for (int qt = 0; qt < QT; qt++) {
         l[qt] += __shfl_xor(l[qt], 16, 64);
@@ -185,7 +218,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
         for (int p = 0; p < WAVES; p++) {
             const float mp = part_ml[p][qt][0][l16], lp = part_ml[p][qt][1][l16];
             if (lp == 0.f) continue;     // a wave without keys for this row counts nothing
-            const float w = mp == m_all ? 1.f : exp_neg(mp - m_all);
+            const float w = mp == m_all ? 1.f : __builtin_amdgcn_exp2f(mp - m_all);
             l_all = fmaf(lp, w, l_all);
 #pragma unroll
             for (int h = 0; h < VH; h++)
@@ -207,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 }
 
 // Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
-// (fp32: e^(m_p - M)), M = max m_p over the parts with keys, parts in index order.  A wave per row: lane p has the weight of part p, every lane D / 64 features.
+// (fp32: references are in base 2, c = 1), M = max m_p over the parts with keys, parts in index order.  A wave per row: lane p has the weight of part p, every lane D / 64 features.
 // Bound by the latency of two loads and, for many rows, by the partial results it reads.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, int parts, float c) {
@@ -221,8 +254,8 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, int
     f32x2 ml = {-__builtin_inff(), 0.f};
     if (lane < parts) ml = *reinterpret_cast<const f32x2*>(a.part + (size_t)a.total_q * a.q_heads * parts * D + (at + lane) * 2);
     const bool any = ml[1] != 0.f;       // (a part without keys for this row: its accumulators were not written)
-    const float m_all = wave_max(any ? ml[0] : -__builtin_inff()), d = ml[0] - m_all;
-    const float w = !any ? 0.f : ml[0] == m_all ? 1.f : sizeof(T) == 4 ? exp_neg(d) : __builtin_amdgcn_exp2f(d * c);
+    const float m_all = wave_max(any ? ml[0] : -__builtin_inff());
+    const float w = !any ? 0.f : ml[0] == m_all ? 1.f : __builtin_amdgcn_exp2f((ml[0] - m_all) * c);
     float l = any ? ml[1] * w : 0.f, x[N];
     l = wave_sum(l);
 #pragma unroll
@@ -249,7 +282,7 @@ int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
     m.parts = 1;
     m.blocks = (int)packed_blocks(a, kPackedRowsMerge);
     HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
-    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid(m), dim3(256), 0, st, m, a.parts, a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid(m), dim3(256), 0, st, m, a.parts, sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
     return hyb_check_launch("packed_attention_merge");
 }
 
@@ -301,10 +334,6 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     a.by_group = packed_divisor((unsigned)a.group);
     a.scale = d.scale > 0.f ? d.scale : (d.head_dim == 64 ? 0.125f : 0.08838834764831845f);
     a.causal = d.causal != 0; a.prescaled = d.prescaled != 0;
-    if (a.prescaled && d.dtype == HYB_F32) {      // the fp32 kernel exponentiates scale x score in base e
-        a.scale = 0.6931471805599453f;
-        a.prescaled = 0;
-    }
     a.q_token = d.q_token_stride * es; a.q_head = d.q_head_stride * es; a.k_token = d.k_token_stride * es; a.k_head = d.k_head_stride * es;
     a.v_token = d.v_token_stride * es; a.v_head = d.v_head_stride * es; a.o_token = d.o_token_stride * es; a.o_head = d.o_head_stride * es;
     HYB_REQUIRE(d.total_k <= 1 << 30, HYB_ERR_SHAPE, "%s: more than 2^30 rows of keys (%d)", who, d.total_k);
