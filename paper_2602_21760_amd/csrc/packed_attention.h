@@ -28,12 +28,14 @@ struct PackedAttnArgs {
     float scale;                                  // > 0; PRE kernels do not use it
     int causal, prescaled;
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
-    int blocks;                                   // row blocks of all sequences, an upper bound (see find_block)
+    int blocks;                                   // row blocks of all sequences, an upper bound (see packed_first_piece)
     int parts;                                    // the keys of a block are cut into up to `parts` parts (see packed_part_tiles); 1: not cut
     int pieces, part_keys;                        // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
     int rests_last;                               // few-rows kernel: pieces that are not full come last (see piece_in_order)
     float* part;                                  // scratch (see below)
-    int xcd_heads, xcd_share;                     // gcd(8, k_heads), 8 / gcd
+    int xcd_heads, xcd_shift, xcd_share;          // gcd(8, k_heads), its logarithm, 8 / gcd
+    unsigned per_head;                            // units of a key head on each of its XCDs (this and the divisors: filled in by packed_grid)
+    PackedDivisor by_head, by_parts;
 };
 
 // Scratch of cut keys.  Blocks of rows that are cut (all but the few-rows kernel): for each (row of q, head) `parts` unnormalised accumulators of head_dim values, then for each `parts` pairs (reference, sum).
@@ -44,9 +46,9 @@ __host__ __device__ inline size_t packed_part_floats(int total_q, int q_heads, i
 // The few-rows kernel numbers pieces of part_keys keys: for each (piece, key head) 16 rows of head_dim values, then for each 16 pairs.
 __host__ __device__ inline size_t packed_piece_rows(int pieces, int k_heads) { return (size_t)pieces * k_heads * 16; }
 
-int hyb_launch_packed_attention_mfma(const PackedAttnArgs& a, int head_dim, hipStream_t st);
-int hyb_launch_packed_attention_few(const PackedAttnArgs& a, int head_dim, hipStream_t st);
-int hyb_launch_packed_attention_f32(const PackedAttnArgs& a, int head_dim, hipStream_t st);
+int hyb_launch_packed_attention_mfma(PackedAttnArgs& a, int head_dim, hipStream_t st);
+int hyb_launch_packed_attention_few(PackedAttnArgs& a, int head_dim, hipStream_t st);
+int hyb_launch_packed_attention_f32(PackedAttnArgs& a, int head_dim, hipStream_t st);
 
 constexpr int kPackedRowsMfma = 128;                                                 // rows of a block: bf16
 constexpr int kPackedRowsFew = 16;                                                   // bf16, few rows per sequence
@@ -64,10 +66,14 @@ inline dim3 packed_grid_of(size_t total) {
     const size_t x = total < ((size_t)1 << 23) ? total : (size_t)1 << 23;
     return dim3((unsigned)x, (unsigned)((total + x - 1) / x));
 }
-__host__ __device__ inline unsigned packed_units(const PackedAttnArgs& a) {
-    return 8u * (unsigned)(a.k_heads / a.xcd_heads) * (unsigned)((a.blocks + a.xcd_share - 1) / a.xcd_share) * (unsigned)a.parts;
+// Grid of a launch over a.blocks row blocks of every key head in a.parts parts; fills in the divisors by which the kernel finds its unit.
+inline dim3 packed_grid(PackedAttnArgs& a) {
+    const unsigned per_head = (unsigned)((a.blocks + a.xcd_share - 1) / a.xcd_share) * (unsigned)a.parts;
+    a.by_head = packed_divisor(per_head);
+    a.by_parts = packed_divisor((unsigned)a.parts);
+    a.per_head = per_head;
+    return packed_grid_of(8 * (size_t)(a.k_heads / a.xcd_heads) * per_head);
 }
-inline dim3 packed_grid(const PackedAttnArgs& a) { return packed_grid_of(packed_units(a)); }
 __device__ __forceinline__ unsigned packed_group_id() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 // Rows of a sequence after the offsets are brought into 0 .. total.
@@ -125,7 +131,9 @@ __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int 
     const int blocks = (int)(((unsigned)(n_q * a.group) + ROWS - 1) / ROWS);
     const int key = min(n_k, (1 << 24) - 1) * 64 + 63 - lane;       // all different
     int before = 0;
-    for (int s = 0; s < a.sequences; s++) before += __builtin_amdgcn_readlane(key, s) > key ? __builtin_amdgcn_readlane(blocks, s) : 0;
+    for (int s0 = 0; s0 < a.sequences; s0 += 8)
+#pragma unroll
+        for (int s = s0; s < s0 + 8; s++) before += __builtin_amdgcn_readlane(key, s) > key ? __builtin_amdgcn_readlane(blocks, s) : 0;     // (lanes without a sequence have no blocks)
     const unsigned long long here = __ballot(rank >= before && rank - before < blocks);
     if (here == 0) return -1;
     const int s = __builtin_ctzll(here);
@@ -137,20 +145,21 @@ __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int 
     return __builtin_amdgcn_readlane(blocks - 1 - (rank - before), s);
 }
 
-// Unit number `id` of a launch; there are packed_units(a), most of them with rows.
+// Unit number `id` of a launch with packed_grid(a), most of them with rows.
 template <int ROWS, bool LONG_FIRST = false>
 __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a, unsigned id) {
     PackedUnit u = {};
     // XCD x (workgroups go round to the 8 XCDs) serves key heads = x mod gcd(8, k_heads), and where XCDs share a head every 8 / gcd-th block of it: the keys of a
     // head stay in as few L2s as possible, and every XCD gets blocks of all lengths.
-    const int xcd = (int)(id % 8), hx = xcd % a.xcd_heads, sx = xcd / a.xcd_heads;
-    unsigned j = id / 8;
-    const unsigned per_head = (unsigned)((a.blocks + a.xcd_share - 1) / a.xcd_share) * (unsigned)a.parts;
-    u.head = hx + a.xcd_heads * (int)(j / per_head);
+    const int xcd = (int)(id % 8), hx = xcd & (a.xcd_heads - 1), sx = xcd >> a.xcd_shift;
+    int j = (int)(id / 8);
+    const int round = packed_div(j, a.by_head);
+    u.head = hx + a.xcd_heads * round;
     if (u.head >= a.k_heads) return u;
-    j %= per_head;
-    u.part = (int)(j % (unsigned)a.parts);
-    int block = (int)(j / (unsigned)a.parts) * a.xcd_share + sx;
+    j -= round * (int)a.per_head;
+    const int b = packed_div(j, a.by_parts);
+    u.part = j - b * a.parts;
+    int block = b * a.xcd_share + sx;
     if (block >= a.blocks) return u;
     int first = 0;
     if (LONG_FIRST && a.sequences > 1 && a.sequences <= 64) {

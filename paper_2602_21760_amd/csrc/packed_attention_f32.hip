@@ -282,7 +282,8 @@ int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
     m.parts = 1;
     m.blocks = (int)packed_blocks(a, kPackedRowsMerge);
     HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
-    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid(m), dim3(256), 0, st, m, a.parts, sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
+    const dim3 grid = packed_grid(m);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D>), grid, dim3(256), 0, st, m, a.parts, sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
     return hyb_check_launch("packed_attention_merge");
 }
 
@@ -340,6 +341,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     HYB_REQUIRE((long long)d.total_q * a.group < (1ll << 31) && packed_blocks(a, 1) * a.k_heads < (1ll << 31) && ((long long)d.total_k / 256 + d.sequences) * a.k_heads < (1ll << 29), HYB_ERR_SHAPE, "%s: too many rows (%d of queries, %d of keys, %d heads)", who, d.total_q, d.total_k, d.q_heads);
     a.xcd_heads = d.k_heads % 8 == 0 ? 8 : d.k_heads % 4 == 0 ? 4 : d.k_heads % 2 == 0 ? 2 : 1;
     a.xcd_share = 8 / a.xcd_heads;
+    a.xcd_shift = a.xcd_heads == 8 ? 3 : a.xcd_heads / 2;
     a.parts = 1;
     // at most 16 rows per sequence: the kernel whose waves split the keys (only the sizes that the caller names can say so; any others are right, too)
     if (d.dtype == HYB_BF16 && d.max_q > 0 && (long long)d.max_q * a.group <= kPackedRowsFew) {
@@ -358,10 +360,11 @@ size_t scratch_bytes(const PackedAttnArgs& a, int head_dim) {
 
 }  // namespace
 
-int hyb_launch_packed_attention_f32(const PackedAttnArgs& a, int head_dim, hipStream_t st) {
+int hyb_launch_packed_attention_f32(PackedAttnArgs& a, int head_dim, hipStream_t st) {
+    const dim3 grid = packed_grid(a);
     HybTraceScope trace("packed_attention_f32", "byte", 8.0 * head_dim * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
-    if (head_dim == 64) hipLaunchKernelGGL(packed_attention_f32_kernel<64>, packed_grid(a), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(packed_attention_f32_kernel<128>, packed_grid(a), dim3(256), 0, st, a);
+    if (head_dim == 64) hipLaunchKernelGGL(packed_attention_f32_kernel<64>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(packed_attention_f32_kernel<128>, grid, dim3(256), 0, st, a);
     return hyb_check_launch("packed_attention_f32");
 }
 

@@ -112,8 +112,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
     // XCD x serves the key heads = x mod gcd(8, k_heads), see packed_unit()
     const unsigned id = packed_group_id();
     const int xcd = (int)(id % 8), per_head = (a.pieces + a.xcd_share - 1) / a.xcd_share;
-    u.head = xcd % a.xcd_heads + a.xcd_heads * (int)(id / 8 / (unsigned)per_head);
-    const int piece = (int)(id / 8 % (unsigned)per_head) * a.xcd_share + xcd / a.xcd_heads;
+    const int round = packed_div((int)(id / 8), a.by_head);
+    u.head = (xcd & (a.xcd_heads - 1)) + a.xcd_heads * round;
+    const int piece = ((int)(id / 8) - round * per_head) * a.xcd_share + (xcd >> a.xcd_shift);
     if (u.head >= a.k_heads || piece >= a.pieces) return;
     if (a.rests_last) {
         piece_in_order(a, piece, u);
@@ -352,8 +353,10 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttnArgs a, floa
 }
 
 template <int D, bool PRE>
-int launch(const PackedAttnArgs& a, hipStream_t st) {
-    const size_t total = 8 * (size_t)(a.k_heads / a.xcd_heads) * ((a.pieces + a.xcd_share - 1) / a.xcd_share);
+int launch(PackedAttnArgs& a, hipStream_t st) {
+    const int per_head = (a.pieces + a.xcd_share - 1) / a.xcd_share;
+    const size_t total = 8 * (size_t)(a.k_heads / a.xcd_heads) * per_head;
+    a.by_head = packed_divisor((unsigned)per_head);
     {
         HybTraceScope trace("packed_attention_few", "byte", 4.0 * D * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
         hipLaunchKernelGGL((packed_attention_few_kernel<D, PRE>), packed_grid_of(total), dim3(256), 0, st, a);
@@ -361,13 +364,14 @@ int launch(const PackedAttnArgs& a, hipStream_t st) {
     const int rc = hyb_check_launch("packed_attention_few");
     if (rc || a.pieces <= a.sequences) return rc;       // no sequence can have two pieces
     HybTraceScope trace("packed_attention_join", "byte", 4.0 * D * (double)a.pieces * a.q_heads, st);
-    hipLaunchKernelGGL((packed_join_kernel<D>), packed_grid(a), dim3(256), 0, st, a, PRE ? 1.f : a.scale * 1.4426950408889634f);
+    const dim3 grid = packed_grid(a);
+    hipLaunchKernelGGL((packed_join_kernel<D>), grid, dim3(256), 0, st, a, PRE ? 1.f : a.scale * 1.4426950408889634f);
     return hyb_check_launch("packed_attention_join");
 }
 
 }  // namespace
 
-int hyb_launch_packed_attention_few(const PackedAttnArgs& a, int head_dim, hipStream_t st) {
+int hyb_launch_packed_attention_few(PackedAttnArgs& a, int head_dim, hipStream_t st) {
     if (head_dim == 64) return a.prescaled ? launch<64, true>(a, st) : launch<64, false>(a, st);
     return a.prescaled ? launch<128, true>(a, st) : launch<128, false>(a, st);
 }
