@@ -111,11 +111,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
     PackedUnit u = {};
     // XCD x serves the key heads = x mod gcd(8, k_heads), see packed_unit()
     const unsigned id = packed_group_id();
-    const int xcd = (int)(id % 8), per_head = (a.pieces + a.xcd_share - 1) / a.xcd_share;
-    const int round = packed_div((int)(id / 8), a.by_head);
-    u.head = (xcd & (a.xcd_heads - 1)) + a.xcd_heads * round;
-    const int piece = ((int)(id / 8) - round * per_head) * a.xcd_share + (xcd >> a.xcd_shift);
-    if (u.head >= a.k_heads || piece >= a.pieces) return;
+    const int xcd = (int)(id % 8), of_head = packed_div((int)(id / 8), a.by_heads), piece = of_head * a.xcd_share + (xcd >> a.xcd_shift);
+    if (piece >= a.pieces) return;
+    u.head = (xcd & (a.xcd_heads - 1)) + a.xcd_heads * ((int)(id / 8) - of_head * (a.k_heads >> a.xcd_shift));
     if (a.rests_last) {
         piece_in_order(a, piece, u);
     } else {
@@ -354,9 +352,8 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttnArgs a, floa
 
 template <int D, bool PRE>
 int launch(PackedAttnArgs& a, hipStream_t st) {
-    const int per_head = (a.pieces + a.xcd_share - 1) / a.xcd_share;
-    const size_t total = 8 * (size_t)(a.k_heads / a.xcd_heads) * per_head;
-    a.by_head = packed_divisor((unsigned)per_head);
+    const size_t total = 8 * (size_t)(a.k_heads / a.xcd_heads) * ((a.pieces + a.xcd_share - 1) / a.xcd_share);
+    a.by_heads = packed_divisor((unsigned)(a.k_heads / a.xcd_heads));
     {
         HybTraceScope trace("packed_attention_few", "byte", 4.0 * D * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
         hipLaunchKernelGGL((packed_attention_few_kernel<D, PRE>), packed_grid_of(total), dim3(256), 0, st, a);
