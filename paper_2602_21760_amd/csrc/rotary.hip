@@ -64,7 +64,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     typedef typename Vec<T>::type vec;
     constexpr int N = Vec<T>::n, PAIRS = HALVES ? N : N / 2;
     extern __shared__ __attribute__((aligned(16))) f32x2 turn[];     // [tile][half] for k, and (FULL) the same times q_scale for q
-    const int t0 = blockIdx.x * a.tile, tokens = min(a.tile, a.tokens - t0);
+    const long long first = (long long)(blockIdx.y * gridDim.x + blockIdx.x) * a.tile;
+    if (first >= a.tokens) return;
+    const int t0 = (int)first, tokens = min(a.tile, a.tokens - t0);
     const int total = tokens * a.units;
     const T* q_in = pinned(static_cast<const T*>(a.q) + (size_t)t0 * a.q_stride);
     const T* k_in = pinned(static_cast<const T*>(a.k) + (size_t)t0 * a.k_stride);
@@ -179,7 +181,9 @@ int launch(RotaryArgs& a, bool halves, int q_heads, int k_heads, hipStream_t st)
     a.unit_magic = magic_of((unsigned)a.units);
     a.head_magic = magic_of((unsigned)a.head_units);
     const bool full = 2 * a.half == a.head_dim;
-    const dim3 grid((unsigned)(((size_t)a.tokens + a.tile - 1) / a.tile));
+    // (a grid dimension holds less than 2^32 threads: what goes beyond 2^23 workgroups goes into the second one)
+    const unsigned groups = (unsigned)(((size_t)a.tokens + a.tile - 1) / a.tile), x = groups < 1u << 23 ? groups : 1u << 23;
+    const dim3 grid(x, (groups + x - 1) / x);
     const size_t lds = (size_t)a.tile * a.half * sizeof(f32x2) * (full ? 2 : 1);
     HybTraceScope trace("rotary", "byte", 2.0 * a.tokens * (q_heads + k_heads) * (double)a.head_dim * sizeof(T), st);
     if (halves && full) hipLaunchKernelGGL((rotary_kernel<T, true, true>), grid, dim3(kThreads), lds, st, a);

@@ -145,6 +145,22 @@ def test_rotary_gradient_is_the_inverse(hb):
     assert abs(diff - (grad * step).sum()) < 2e-3
 
 
+def test_rotary_more_workgroups_than_one_grid_dimension_holds(hb):
+    """2^28 + 37 tokens of one small head: more than 2^24 workgroups of 256 threads, 8.6 GB."""
+    tokens = 2 ** 28 + 37
+    q = torch.ones(tokens, 1, 16, device="cuda", dtype=torch.bfloat16)
+    p = torch.arange(tokens, device="cuda", dtype=torch.int32).remainder_(1009)[:, None]
+    hb.hyb_rotary(hb.rotary_desc(q, None, (16,)), p, q)
+    rows = torch.cat([torch.arange(40), torch.tensor([2 ** 27 - 1, 2 ** 27, 2 ** 27 + 1, 123456789]), torch.arange(2 ** 28 - 40, tokens)])
+    at = rows.cuda()
+    x = np.ones((len(rows), 1, 16))
+    want = P.rotary(x, p[at].cpu().numpy(), (16,))
+    assert (np.abs(host(q[at]) - want) <= P.rotary_bound(x, 2.0 ** -8, axis_dims=(16,))(want)).all()
+    # every row turned once and by its own angle: rows of one position are alike
+    same = q[1009 * 7 + 5:1009 * 7 + 5 + 1009 * 266000].view(266000, 1009, 16)
+    assert bool((same == same[0]).all())
+
+
 def test_rotary_binding_refusals(hb):
     q = torch.zeros(8, 2, 64, device="cuda", dtype=torch.bfloat16)
     p = torch.zeros(8, 1, dtype=torch.int32, device="cuda")
@@ -218,6 +234,31 @@ def test_attention_lengths(hb, dt, heads, causal):
             assert not got[0][3:-3].any()                  # nobody sees a key
             continue
         _check(dt, *got)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_more_sequences_than_lanes(hb, dt, causal):
+    lens = [(7 * i) % 61 for i in range(150)]
+    _check(dt, *_attention(hb, dt, lens, [n + i % 3 for i, n in enumerate(lens)], 6, 3, 64, causal=causal, spare=2, layout="kv"))
+
+
+@pytest.mark.parametrize("new", [0, 1])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_broadcast_keys(hb, dt, new):
+    """Keys and values that are one row for all tokens, or one head for all heads (strides of 0): every query gets the mean of what it sees."""
+    n = 300
+    q = dev(synth.normal(1, (new or n, 4, 64), 1.0, dt), tdt(dt))
+    k, v = (dev(synth.normal(s, (n, 1, 64), 1.0, dt), tdt(dt)) for s in (2, 3))
+    cu_q, cu_k = _offsets([new or n]), _offsets([n])
+    for name, kk, vv in (("tokens", k[:1].expand(n, 2, 64), v[:1].expand(n, 2, 64)), ("heads", k.expand(n, 2, 64), v.expand(n, 2, 64))):
+        o = torch.full_like(q, 7.0)
+        desc = hb.packed_attention_desc(q, kk, vv, o, cu_q, new or n, n)
+        ws = torch.empty(hb.hyb_packed_attention_workspace_bytes(desc), device="cuda", dtype=torch.uint8)
+        hb.hyb_packed_attention(desc, q, kk, vv, o, cu_q, cu_k, ws)
+        args = host(q), host(kk.contiguous()), host(vv.contiguous()), cu_q.cpu().numpy(), cu_k.cpu().numpy()
+        want = P.packed_attention(*args)
+        assert (np.abs(host(o) - want) <= P.packed_attention_bound(*args, dt == "bf16")).all(), name
 
 
 @pytest.mark.parametrize("layout", ["fused", "heads", "kv"])
