@@ -403,22 +403,25 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
         out_of_range |= !(zero[0] + zero[1] + zero[2] + zero[3] == 0.f);
         const int wave_bad = __any(out_of_range) ? 1 : 0;
         if (lane == 0) wave_flags[wave] = wave_bad;
-        __syncthreads();                                     // ... and every wave is done with the tile buffers
+        __syncthreads();                                     // ... and every wave is done with the tile buffers, in which the wave's 32 rows of the result are turned
         const bool again = (wave_flags[0] | wave_flags[1] | wave_flags[2] | wave_flags[3]) != 0;
         if (again) {
             clear(-__builtin_inff());
             key_loop(std::false_type{});
+            __syncthreads();
         }
     }
 
     const int le = lane_again(), l16e = le % 16, q4e = le / 16;
+    // results leave through LDS, whole rows with 16 bytes a lane (straight from the accumulators, 8 bytes a lane in 32-byte pieces: 1 to 2 % slower at head_dim 128, the same at 64)
+    unsigned char* out = &smem[0][0] + wave * 32 * ROWB;
 #pragma unroll
     for (int qt = 0; qt < 2; qt++) {
         const float l = row_total(l_run[qt]);
-        if (wave * 32 + qt * 16 + l16e >= u.rows) continue;
         const int row = u.row0 + wave * 32 + qt * 16 + l16e;
         const int tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
         if (a.parts > 1) {
+            if (wave * 32 + qt * 16 + l16e >= u.rows) continue;
             const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
             if (q4e == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
             if (l != 0.f) {                                  // (nothing to merge otherwise)
@@ -428,10 +431,21 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
             continue;
         }
         const float inv = l == 0.f ? 0.f : 1.0f / l;         // no key with a score above minus infinity: zeros
-        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 8 * q4e;
+        const int r = qt * 16 + l16e;
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
-            *reinterpret_cast<bf16x4*>(op + dt * 32) = bf16x4{(bf16_t)(o[dt][qt][0] * inv), (bf16_t)(o[dt][qt][1] * inv), (bf16_t)(o[dt][qt][2] * inv), (bf16_t)(o[dt][qt][3] * inv)};
+            *reinterpret_cast<bf16x4*>(out + r * ROWB + (((2 * dt + q4e / 2) ^ (r % SLOTS)) * 16) + (q4e % 2) * 8) =
+                bf16x4{(bf16_t)(o[dt][qt][0] * inv), (bf16_t)(o[dt][qt][1] * inv), (bf16_t)(o[dt][qt][2] * inv), (bf16_t)(o[dt][qt][3] * inv)};
+    }
+    if (a.parts > 1) return;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 32 / CHUNK_ROWS; j++) {
+        const int r = j * CHUNK_ROWS + le / SLOTS, row0 = wave * 32 + r;
+        if (row0 >= u.rows) continue;
+        const int row = u.row0 + row0, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
+        *reinterpret_cast<bf16x8*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + (le % SLOTS) * 16) =
+            *reinterpret_cast<const bf16x8*>(out + r * ROWB + (((le % SLOTS) ^ (r % SLOTS)) * 16));
     }
 }
 
