@@ -28,7 +28,7 @@
  *    else is in the batch (no floating-point atomics).  How many samples there are may decide its last bits where bf16
  *    launches split sums by their size: attention with scratch (the _ws and _prescaled forms and hyb_block_forward cut some query
  *    blocks along the keys), and the stage block of the U-Net shape with 512 channels or more, or with a long context feature
- *    axis (GEMMs split along k).
+ *    axis (GEMMs split along k); attention over packed batches cuts keys by the sizes of the whole batch.
  */
 #ifndef HYB_H
 #define HYB_H
@@ -344,7 +344,7 @@ int hyb_rotary(const hyb_rotary_desc* desc, const int* positions, const void* q,
 typedef struct {
     int sequences;
     int total_q, total_k;                            /* rows of q and o, rows of k and v */
-    int max_q, max_k;                                /* most queries / keys of one sequence, 0: unknown.  They choose the way to the result (splits), not the result */
+    int max_q, max_k;                                /* most queries / keys of one sequence, 0: unknown.  They choose the way to the result (single tokens want both), not the result */
     int q_heads, k_heads;                            /* q_heads % k_heads == 0: query head h reads key head h / (q_heads / k_heads) */
     int head_dim;                                    /* 64 or 128 */
     float scale;                                     /* <= 0 means 1 / sqrt(head_dim) */
@@ -361,10 +361,12 @@ typedef struct {
  * text, whole prompts (causal), new tokens at the end of longer caches (causal with n_q < n_k), single queries.
  * offsets_q, offsets_k: device int[sequences + 1].  q, o: device, feature i of head h of row t at t * token_stride + h * head_stride + i; k, v
  * likewise with k_heads heads.  Token-major and head-major tensors and slices of joint projections are all of this form.
- * A query that sees no key (its sequence has none, or causal with n_q > n_k) gets zeros.  What a key holds that a query does not see, infinities and
- * NaN among it, does not reach that query.  Rows of o that belong to no sequence are left as they are.
+ * A query that sees no key (its sequence has none, or causal with n_q > n_k) or only scores of minus infinity gets zeros.  What a key holds that a query
+ * does not see, infinities and NaN among it, does not reach that query.  Rows of o that belong to no sequence are left as they are.  o shares no element
+ * with q, k or v; of these several may be one tensor, and strides of 0 are allowed.  Scores, the normaliser and the sums over values are fp32 (sums unnormalised: finite
+ * while 2^8 times the number of keys times the largest value is below 2^128); bf16 rounds every probability once for its product with the values, and the result.
  * Calls with few query rows cut the keys into parts that other workgroups take and merge the unnormalised partial results in a second kernel, in a
- * fixed order: deterministic, but the number of parts, which follows from the descriptor alone, may decide last bits.
+ * fixed order: deterministic, but the cut, which follows from the descriptor and the offsets alone, may decide last bits.
  * workspace: device, >= hyb_packed_attention_workspace_bytes(desc) (0: may be NULL), contents irrelevant; calls that overlap in time need one each. */
 int hyb_packed_attention(const hyb_packed_attention_desc* desc, const void* q, const void* k, const void* v, void* o,
                          const int* offsets_q, const int* offsets_k, void* workspace, size_t workspace_bytes, void* stream);
