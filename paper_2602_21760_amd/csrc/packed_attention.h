@@ -28,9 +28,10 @@ struct PackedAttnArgs {
     float scale;                                  // > 0; PRE kernels do not use it
     int causal, prescaled;
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
-    int blocks;                                   // row blocks of all sequences, an upper bound (see packed_first_piece)
+    int blocks;                                   // row blocks of all sequences, an upper bound (see packed_find)
     int parts;                                    // the keys of a block are cut into up to `parts` parts (see packed_part_tiles); 1: not cut
     int pieces, part_keys;                        // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
+    PackedDivisor by_piece;                       // part_keys
     int rests_last;                               // few-rows kernel: pieces that are not full come last (see piece_in_order)
     float* part;                                  // scratch (see below)
     int xcd_heads, xcd_shift, xcd_share;          // gcd(8, k_heads), its logarithm, 8 / gcd
@@ -79,26 +80,6 @@ __device__ __forceinline__ unsigned packed_group_id() { return blockIdx.y * grid
 // Rows of a sequence after the offsets are brought into 0 .. total.
 __device__ __forceinline__ int packed_offset(const int* offsets, int s, int total) { return min(max(offsets[s], 0), total); }
 
-// Pieces of sequences are numbered without a table: with `per` pieces' worth of rows (a block of query rows, a part of the keys) sequence s begins at number
-// floor(first row / per) + s, which leaves every sequence at least as many numbers as it has pieces, and at least one (floor(x + n) - floor(x) + 1 >=
-// ceil(n)); numbers left over have no rows.  The sequence of a number is the last one that begins at or before it, found by all lanes of the wave at
-// once, 64 candidates a step.
-__device__ __forceinline__ int packed_first_piece(const int* offsets, int s, int total, int mul, int per) {
-    return (int)((long long)packed_offset(offsets, s, total) * mul / per) + s;
-}
-__device__ __forceinline__ int packed_sequence_of(const int* offsets, int sequences, int total, int mul, int per, int piece) {
-    const int lane = threadIdx.x % 64;
-    int lo = 0, len = sequences;
-    while (len > 1) {
-        const int step = (len + 63) / 64, s = min(lo + lane * step, sequences - 1);
-        const int count = __popcll(__ballot(lane * step < len && packed_first_piece(offsets, s, total, mul, per) <= piece));
-        const int at = count > 0 ? count - 1 : 0;
-        lo += at * step;
-        len = min(step, len - at * step);
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
-
 // What a workgroup works on; rows == 0: nothing.
 struct PackedUnit {
     int head, part;              // key head, part of the keys
@@ -110,8 +91,53 @@ struct PackedUnit {
 __device__ __forceinline__ void packed_rows_of(const PackedAttnArgs& a, int s, PackedUnit& u) {
     u.q0 = packed_offset(a.offsets_q, s, a.total_q);
     u.k0 = packed_offset(a.offsets_k, s, a.total_k);
-    u.n_q = packed_offset(a.offsets_q, s + 1, a.total_q) - u.q0;
+    u.n_q = max(packed_offset(a.offsets_q, s + 1, a.total_q) - u.q0, 0);
     u.n_k = max(packed_offset(a.offsets_k, s + 1, a.total_k) - u.k0, 0);
+}
+
+// Up to 64 sequences: lane s holds sequence s (lanes without one: no rows), so that one trip to memory finds a unit.
+__device__ __forceinline__ PackedUnit packed_lanes(const PackedAttnArgs& a) {
+    PackedUnit mine = {};
+    const int lane = threadIdx.x % 64;
+    if (lane < a.sequences) packed_rows_of(a, lane, mine);
+    return mine;
+}
+__device__ __forceinline__ void packed_take(const PackedUnit& lanes, int s, PackedUnit& u) {
+    u.sequence = s;
+    u.q0 = __builtin_amdgcn_readlane(lanes.q0, s);
+    u.k0 = __builtin_amdgcn_readlane(lanes.k0, s);
+    u.n_q = __builtin_amdgcn_readlane(lanes.n_q, s);
+    u.n_k = __builtin_amdgcn_readlane(lanes.n_k, s);
+}
+
+// Pieces of sequences are numbered without a table: with `per` pieces' worth of rows (a block of query rows, a part of the keys) sequence s begins at number
+// floor(first row / per) + s, which leaves every sequence at least as many numbers as it has pieces, and at least one (floor(x + n) - floor(x) + 1 >=
+// ceil(n)); numbers left over have no rows.  The sequence of a number is the last one that begins at or before it, found by all lanes of the wave at
+// once, 64 candidates a step.
+// KEYS: pieces are of the keys, otherwise of the rows of queries; number: floor(first row / per).  Fills in the sequence's rows and returns the number of its first piece.
+template <bool KEYS, typename N>
+__device__ __forceinline__ int packed_find(const PackedAttnArgs& a, int piece, PackedUnit& u, N number) {
+    const int lane = threadIdx.x % 64;
+    if (a.sequences <= 64) {
+        const PackedUnit lanes = packed_lanes(a);
+        const int first = number(KEYS ? lanes.k0 : lanes.q0) + lane;
+        const int s = max(__popcll(__ballot(lane < a.sequences && first <= piece)) - 1, 0);
+        packed_take(lanes, s, u);
+        return __builtin_amdgcn_readlane(first, s);
+    }
+    const int* offsets = KEYS ? a.offsets_k : a.offsets_q;
+    const int total = KEYS ? a.total_k : a.total_q;
+    int lo = 0, len = a.sequences;
+    while (len > 1) {
+        const int step = (len + 63) / 64, s = min(lo + lane * step, a.sequences - 1);
+        const int count = __popcll(__ballot(lane * step < len && number(packed_offset(offsets, s, total)) + s <= piece));
+        const int at = count > 0 ? count - 1 : 0;
+        lo += at * step;
+        len = min(step, len - at * step);
+    }
+    u.sequence = __builtin_amdgcn_readfirstlane(lo);
+    packed_rows_of(a, u.sequence, u);
+    return number(KEYS ? u.k0 : u.q0) + u.sequence;
 }
 
 // The rank-th block when sequences come in the order of decreasing numbers of keys (up to 64 of them) and a sequence's late blocks first, which are the long ones
@@ -121,15 +147,9 @@ __device__ __forceinline__ void packed_rows_of(const PackedAttnArgs& a, int s, P
 template <int ROWS>
 __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int rank, PackedUnit& u) {
     const int lane = threadIdx.x % 64;
-    int q0 = 0, k0 = 0, n_q = 0, n_k = 0;
-    if (lane < a.sequences) {
-        q0 = packed_offset(a.offsets_q, lane, a.total_q);
-        k0 = packed_offset(a.offsets_k, lane, a.total_k);
-        n_q = max(packed_offset(a.offsets_q, lane + 1, a.total_q) - q0, 0);
-        n_k = max(packed_offset(a.offsets_k, lane + 1, a.total_k) - k0, 0);
-    }
-    const int blocks = (int)(((unsigned)(n_q * a.group) + ROWS - 1) / ROWS);
-    const int key = min(n_k, (1 << 24) - 1) * 64 + 63 - lane;       // all different
+    const PackedUnit lanes = packed_lanes(a);
+    const int blocks = (int)(((unsigned)(lanes.n_q * a.group) + ROWS - 1) / ROWS);
+    const int key = min(lanes.n_k, (1 << 24) - 1) * 64 + 63 - lane;       // all different
     int before = 0;
     for (int s0 = 0; s0 < a.sequences; s0 += 8)
 #pragma unroll
@@ -137,11 +157,7 @@ __device__ __forceinline__ int packed_ranked_block(const PackedAttnArgs& a, int 
     const unsigned long long here = __ballot(rank >= before && rank - before < blocks);
     if (here == 0) return -1;
     const int s = __builtin_ctzll(here);
-    u.sequence = s;
-    u.q0 = __builtin_amdgcn_readlane(q0, s);
-    u.k0 = __builtin_amdgcn_readlane(k0, s);
-    u.n_q = __builtin_amdgcn_readlane(n_q, s);
-    u.n_k = __builtin_amdgcn_readlane(n_k, s);
+    packed_take(lanes, s, u);
     return __builtin_amdgcn_readlane(blocks - 1 - (rank - before), s);
 }
 
@@ -168,12 +184,10 @@ __device__ __forceinline__ PackedUnit packed_unit(const PackedAttnArgs& a, unsig
         if (block < 0) return u;
     } else {
         block = a.blocks - 1 - block;        // late blocks first: with a causal mask they are the long ones
-        u.sequence = packed_sequence_of(a.offsets_q, a.sequences, a.total_q, a.group, ROWS, block);
-        first = packed_first_piece(a.offsets_q, u.sequence, a.total_q, a.group, ROWS);
+        first = packed_find<false>(a, block, u, [&](int q0) { return (int)((long long)q0 * a.group / ROWS); });
         if (first > block) return u;
-        packed_rows_of(a, u.sequence, u);
     }
-    const long long all = (long long)max(u.n_q, 0) * a.group, row0 = (long long)(block - first) * ROWS;
+    const long long all = (long long)u.n_q * a.group, row0 = (long long)(block - first) * ROWS;
     u.rows = (int)max(min(all - row0, (long long)ROWS), 0ll);
     u.row0 = (int)row0;           // (meaningful when rows > 0: below total_q * group, which the launcher keeps below 2^31)
     return u;

@@ -310,6 +310,7 @@ void choose_pieces(PackedAttnArgs& a, int max_k, int slots) {
     const bool alike = max_k <= 2048 && 4ll * a.sequences * max_k <= 7ll * a.total_k && 3ll * a.total_k * a.k_heads >= (long long)max_k * slots;
     if (max_k > 0 && (max_k <= len || alike)) len = 1 << 30;
     a.part_keys = (int)len;
+    a.by_piece = packed_divisor((unsigned)len);
     a.pieces = (int)(a.total_k / len) + a.sequences;
     a.rests_last = a.sequences <= 64 && (long long)a.pieces * a.k_heads > slots;
     a.blocks = (int)packed_blocks(a, 1);       // of the join

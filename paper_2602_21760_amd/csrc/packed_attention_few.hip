@@ -6,7 +6,7 @@
 // place is under way during this tile's arithmetic.  (Keys loaded straight to registers, 64 bytes of a row per instruction, reach 10 % less bandwidth.)  Running maximum and normaliser per wave; the four partial results are joined in LDS, in a
 // fixed order, and those of a sequence's parts by a second kernel.
 //
-// Caches are of all lengths, so workgroups are numbered by pieces of part_keys keys (as blocks of rows are elsewhere, see packed_sequence_of): a launch holds
+// Caches are of all lengths, so workgroups are numbered by pieces of part_keys keys (as blocks of rows are elsewhere, see packed_find): a launch holds
 // at most one workgroup without work per sequence and head, and long sequences are spread over as many workgroups as they have pieces.
 #include "packed_attention.h"
 
@@ -59,14 +59,8 @@ __device__ __forceinline__ void v_fragments(unsigned at, bf16x4 (&vh)[D / 16][2]
 // holds sequence s.  Fills in the sequence's rows and the part (-1: there are fewer pieces).
 __device__ __forceinline__ void piece_in_order(const PackedAttnArgs& a, int piece, PackedUnit& u) {
     const int lane = threadIdx.x % 64;
-    int q0 = 0, k0 = 0, n_q = 0, n_k = 0;
-    if (lane < a.sequences) {
-        q0 = packed_offset(a.offsets_q, lane, a.total_q);
-        k0 = packed_offset(a.offsets_k, lane, a.total_k);
-        n_q = max(packed_offset(a.offsets_q, lane + 1, a.total_q) - q0, 0);
-        n_k = max(packed_offset(a.offsets_k, lane + 1, a.total_k) - k0, 0);
-    }
-    const int full = n_k / a.part_keys, rest = n_k - full * a.part_keys;
+    const PackedUnit lanes = packed_lanes(a);
+    const int full = packed_div(lanes.n_k, a.by_piece), rest = lanes.n_k - full * a.part_keys;
     int end = full;              // full pieces up to and with this sequence
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
@@ -92,14 +86,10 @@ __device__ __forceinline__ void piece_in_order(const PackedAttnArgs& a, int piec
             before += __popcll(these);
         }
         s = __builtin_ctzll(__ballot(size >= 0 && rank == left));
-        part = __builtin_amdgcn_readlane(rest > 0 || n_k == 0 ? full : -1, s);
+        part = __builtin_amdgcn_readlane(rest > 0 || lanes.n_k == 0 ? full : -1, s);
     }
-    u.sequence = s;
+    packed_take(lanes, s, u);
     u.part = part;
-    u.q0 = __builtin_amdgcn_readlane(q0, s);
-    u.k0 = __builtin_amdgcn_readlane(k0, s);
-    u.n_q = __builtin_amdgcn_readlane(n_q, s);
-    u.n_k = __builtin_amdgcn_readlane(n_k, s);
 }
 
 template <int D, bool PRE>
@@ -117,11 +107,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
     if (a.rests_last) {
         piece_in_order(a, piece, u);
     } else {
-        u.sequence = packed_sequence_of(a.offsets_k, a.sequences, a.total_k, 1, a.part_keys, piece);
-        u.part = piece - packed_first_piece(a.offsets_k, u.sequence, a.total_k, 1, a.part_keys);
-        packed_rows_of(a, u.sequence, u);
+        u.part = piece - packed_find<true>(a, piece, u, [&](int k0) { return packed_div(k0, a.by_piece); });
     }
-    const int rows = max(u.n_q, 0) * a.group, parts = rows <= BQ ? (u.n_k + a.part_keys - 1) / a.part_keys : 1;
+    const int rows = u.n_q * a.group, parts = rows <= BQ ? packed_div(u.n_k + a.part_keys - 1, a.by_piece) : 1;
     if (rows == 0 || u.part < 0 || u.part >= max(parts, 1)) return;
     const int lane = threadIdx.x % 64, l16 = lane % 16, q4 = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -286,7 +274,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_attention_few_ker
             }
             const int rr = u.row0 + r, tk = packed_div(rr, a.by_group), head = u.head * a.group + (rr - tk * a.group);
             if (parts > 1) {
-                const size_t place = (size_t)(u.k0 / a.part_keys + u.sequence + u.part), at = (place * a.k_heads + u.head) * BQ + r;     // (packed_first_piece + part)
+                const size_t place = (size_t)(packed_div(u.k0, a.by_piece) + u.sequence + u.part), at = (place * a.k_heads + u.head) * BQ + r;     // (the piece's number)
                 if (f == 0) *reinterpret_cast<f32x2*>(a.part + packed_piece_rows(a.pieces, a.k_heads) * D + at * 2) = f32x2{m_all, l};
                 *reinterpret_cast<f32x4*>(a.part + at * D + f) = x;
             } else {
@@ -308,11 +296,11 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttnArgs a, floa
     __shared__ float weight[64];
     const PackedUnit u = packed_unit<1>(a, packed_group_id());
     if (u.rows == 0 || u.n_q * a.group > BQ) return;
-    const int parts = (u.n_k + a.part_keys - 1) / a.part_keys;
+    const int parts = packed_div(u.n_k + a.part_keys - 1, a.by_piece);
     if (parts <= 1) return;              // (written already)
     const int tid = threadIdx.x, f = tid % F, g = tid / F;
     const int row = u.row0, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
-    const size_t at = ((size_t)packed_first_piece(a.offsets_k, u.sequence, a.total_k, 1, a.part_keys) * a.k_heads + u.head) * BQ + row, step = (size_t)a.k_heads * BQ;
+    const size_t at = ((size_t)(packed_div(u.k0, a.by_piece) + u.sequence) * a.k_heads + u.head) * BQ + row, step = (size_t)a.k_heads * BQ;
     const f32x2* ml = reinterpret_cast<const f32x2*>(a.part + packed_piece_rows(a.pieces, a.k_heads) * D) + at;
     const float* o = a.part + at * D + 4 * f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
