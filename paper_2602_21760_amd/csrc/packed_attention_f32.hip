@@ -9,7 +9,7 @@
 // with 382 vector instructions beside the 128 MFMAs of a tile, no better with waves of different priority).  So a tile has few others: a probability is one fma and one
 // v_exp_f32, 2^(c score - reference), whose error is that of an argument near 0 wherever the probability counts; masks, maxima across lanes and rescaling only where a tile asks for them;
 // offsets of buffer loads that no tile changes.  One sequence of 4096, 8 heads: head_dim 64 127 TFLOP/s, 128 107 (a large library product in fp32 reaches 139); 16 rows at head_dim 64 110.
-// Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles and by the last round (314, 1302 and 259 tokens, 12 / 4 heads of 64: 65 us, 88 TFLOP/s).
+// Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles and by the last round (314, 1302 and 259 tokens, 12 / 4 heads of 64: 57 to 65 us from card to card, 88 to 100 TFLOP/s).
 #include "packed_attention.h"
 
 namespace {

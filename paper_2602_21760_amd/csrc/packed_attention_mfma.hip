@@ -17,8 +17,9 @@
 // result is not finite, the workgroup starts over in the same way as for sums out of range, and the second attempt searches every tile that not all rows see, zeroes such
 // values in the fragments and adds them to the rows that do see them.  (The search in the first attempt takes 3 to 9 % of launches over short sequences.)
 //
-// Bound by what the matrix cores sustain beside the softmax (16717 tokens, 24 heads of 64: 1170 TFLOP/s; 8192 tokens, 32 / 8 heads of 128: 1300, causal 1255) and, for short sequences, by the 5 us
-// that a workgroup takes before and after its key loop: 4 workgroups a CU at head_dim 64, 3 at 128.  (64 keys a tile at head_dim 128 take 200 registers, 2 workgroups a CU: 2 % slower on
+// Bound by what the matrix cores sustain beside the softmax (16717 tokens, 24 heads of 64: 1180 TFLOP/s; 8192 tokens, 32 / 8 heads of 128: 1300, causal 1255) and, for short sequences, by the 7 us
+// that a workgroup takes before and after its key loop (24 prompts of 33 to 4000: 2 to find its unit, 2 for the first tile, 3 for the result, 24 for the keys; 880 TFLOP/s): 4 workgroups a CU
+// at head_dim 64, 3 at 128.  (64 keys a tile at head_dim 128 take 200 registers, 2 workgroups a CU: 2 % slower on
 // 8192 tokens, 8 % on prompts of 33 to 4000, 14 % on prompts of 300.  Workgroups that walk through several units, the next one's first tile under way, from a queue filled by a
 // kernel before: as fast at head_dim 128, 20 % slower at 64.)
 #include "packed_attention.h"
