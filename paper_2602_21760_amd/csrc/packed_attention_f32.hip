@@ -287,17 +287,31 @@ int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
     return hyb_check_launch("packed_attention_merge");
 }
 
-// How the keys are cut: `parts` workgroups per block of rows where a launch's row blocks would leave most of the chip idle (the end of a long prompt); each block deals its own keys out to them.
-// max_k == 0: the keys of all sequences bound one sequence's.  slots: workgroups that the chip holds.
-void choose_parts(PackedAttnArgs& a, int max_k, int slots) {
-    const long long units = (long long)a.blocks * a.k_heads;
-    const int keys = max_k > 0 && max_k < a.total_k ? max_k : a.total_k;
-    if (units == 0 || units * 2 > slots || keys <= 512) return;
-    long long parts = slots / units;
-    if (parts > kPackedMaxParts) parts = kPackedMaxParts;
-    const long long most = (keys + kPackedPartKeys - 1) / kPackedPartKeys;
-    a.parts = (int)(parts < most ? parts : most);
+// How many parts the keys of a block are cut into; each block deals its own keys out to them.  The least over an estimate of a launch's length in us: the longest part's keys at the pace of a
+// workgroup that is alone on its CU, or all blocks' at the pace of a full chip, whatever is longer; the start of the workgroups; the merge: a launch, a share per row, the partial results that are
+// written and read.  Fitted to 302 launches of 1 to 64 sequences of 50 to 9000 keys, in caches and out of them, each in 1 to 32 parts: 1 % above the best on average, 3 % where the keys come from
+// memory (as many parts as fill the chip: 7 and 9 %; 10 heads of 64, 8 sequences of 648: not cut 21 us, in two 43; 17 tokens over 2031 to 3695 keys, 16 / 8 heads of 128: 69 and, in six, 22).
+// Never more than the chip holds at once.  max_k == 0: half as many again as the mean; it decides the number of parts only.
+void choose_parts(PackedAttnArgs& a, int max_k, bool f32, int head_dim) {
+    const double mean = (double)a.total_k / a.sequences, most = max_k > 0 ? max_k : 1.5 * mean, keys = most < a.total_k ? most : a.total_k;
+    if (!f32 && keys <= 512) return;                // (bf16 blocks of so few keys gain nothing: 10.5 us, cut 12.9)
+    const double key = f32 ? (head_dim == 64 ? 0.015 : 0.025) : head_dim == 64 ? 0.009 : 0.014;
+    const double blocks = ((double)a.total_q * a.group / (f32 ? packed_rows_f32(head_dim) : kPackedRowsMfma) + 0.5 * a.sequences) * a.k_heads;
+    const double seen = a.causal && a.total_q == a.total_k ? 0.5 * mean : mean, all = blocks * seen * key / (hyb_cu_count() * (f32 ? 1.2 : 1.6));
+    const double rows = (double)a.total_q * a.q_heads;
+    double best = 0;
+    const int slots = hyb_cu_count() * (f32 ? 2 : head_dim == 64 ? 4 : 3);
+    for (int parts = 1; parts <= kPackedMaxParts && (parts == 1 || ((parts - 1) * kPackedPartKeys < keys && parts * blocks <= slots)); parts++) {
+        const double share = keys / parts > kPackedPartKeys ? keys / parts : kPackedPartKeys, own = (parts == 1 ? keys : share) * key;
+        const double merge = parts == 1 ? 0 : 2.4 + rows * (0.2e-3 + 0.1e-3 * parts * head_dim / 64);
+        const double us = (own > all ? own : all) + 0.003 * blocks * parts + merge;
+        if (parts == 1 || us < best) {
+            best = us;
+            a.parts = parts;
+        }
+    }
 }
+
 // Pieces of the few-rows kernel: all keys dealt out over the chip, two pieces for every workgroup that fits it (one: 11 % slower over caches of 100 to 8000 keys, three: the same), of at
 // least 256 keys (8000 keys of one sequence, 8 heads of 128: 11.7 us; of 512: 13.0), or 512 where the sequences alone fill the chip.  Sequences of which the caller says that none is
 // longer than a piece are one piece each, whatever their length, and need no join.  So are those of up to 2048 keys and much the same length that keep a third of the chip busy: what
@@ -349,7 +363,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
         choose_pieces(a, d.max_k, hyb_cu_count() * (d.head_dim == 64 ? 4 : 2));
     } else {
         a.blocks = (int)packed_blocks(a, d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim));
-        choose_parts(a, d.max_k, hyb_cu_count() * (d.dtype == HYB_F32 ? 2 : d.head_dim == 64 ? 4 : 3));
+        if (d.sequences > 0) choose_parts(a, d.max_k, d.dtype == HYB_F32, d.head_dim);
     }
     return HYB_OK;
 }
