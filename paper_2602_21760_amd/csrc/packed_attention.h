@@ -53,8 +53,7 @@ int hyb_launch_packed_attention_f32(PackedAttnArgs& a, int head_dim, hipStream_t
 
 constexpr int kPackedRowsMfma = 128;                                                 // rows of a block: bf16
 constexpr int kPackedRowsFew = 16;                                                   // bf16, few rows per sequence
-constexpr int kPackedRowsMerge = 4;                                                  // merge of cut keys: a wave per row
-constexpr int kPackedMaxParts = 64;                                                  // its lanes hold a part's weight each
+constexpr int kPackedMaxParts = 64;
 constexpr int kPackedPartKeys = 256;                                                 // least keys of a part
 constexpr int packed_tile_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }    // keys of its LDS tiles
 constexpr int packed_rows_f32(int head_dim) { return head_dim == 64 ? 32 : 16; }     // fp32

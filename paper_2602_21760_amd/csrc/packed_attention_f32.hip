@@ -240,56 +240,71 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 }
 
 // Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
-// (fp32: references are in base 2, c = 1), M = max m_p over the parts with keys, parts in index order.  A wave per row: lane p has the weight of part p, every lane D / 64 features.
-// Bound by the latency of two loads and, for many rows, by the partial results it reads.
+// (fp32: references are in base 2, c = 1), M = max m_p over the parts with keys, parts in index order.  D / 4 lanes per row, four features each; lane f has the weights of parts f, f + D / 4, ...
+// Rows are those of all offsets (they do not decrease), so no sequence has to be found: one trip to memory for the pairs and the first accumulators, one for every eight more.  Bound
+// by that latency and, for many rows, by the partial results it reads.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, int parts, float c) {
-    constexpr int N = D / 64;
-    const PackedUnit u = packed_unit<kPackedRowsMerge>(a, packed_group_id());
-    const int lane = threadIdx.x % 64, r = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (r >= u.rows) return;
-    const int row = u.row0 + r, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
-    const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * parts;
-    const float* o = a.part + at * D + lane * N;
-    f32x2 ml = {-__builtin_inff(), 0.f};
-    if (lane < parts) ml = *reinterpret_cast<const f32x2*>(a.part + (size_t)a.total_q * a.q_heads * parts * D + (at + lane) * 2);
-    const bool any = ml[1] != 0.f;       // (a part without keys for this row: its accumulators were not written)
-    const float m_all = wave_max(any ? ml[0] : -__builtin_inff());
-    const float w = !any ? 0.f : ml[0] == m_all ? 1.f : __builtin_amdgcn_exp2f((ml[0] - m_all) * c);
-    float l = any ? ml[1] * w : 0.f, x[N];
-    l = wave_sum(l);
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, PackedDivisor by_q_heads, float c) {
+    constexpr int G = D / 4, ROWS = 64 / G, E = kPackedMaxParts / G, U = 8;
+    typedef T tx4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x % 64, g = lane / G, f = lane % G, parts = a.parts;
+    const unsigned all = (unsigned)a.total_q * (unsigned)a.q_heads, row = (packed_group_id() * 4 + threadIdx.x / 64) * ROWS + g, r = min(row, all - 1);
+    const float* o = a.part + (size_t)r * parts * D + 4 * f;
+    const f32x2* pairs = reinterpret_cast<const f32x2*>(a.part + (size_t)all * parts * D) + (size_t)r * parts;
+    f32x2 e[E];
 #pragma unroll
-    for (int e = 0; e < N; e++) x[e] = 0.f;
-    const unsigned long long with_keys = __ballot(any);
-#pragma unroll 8
-    for (int p = 0; p < parts; p++) {
-        const float wp = __shfl(w, p, 64);
-        float v[N];
+    for (int i = 0; i < E; i++) e[i] = pairs[min(f + i * G, parts - 1)];
+    const int begin = packed_offset(a.offsets_q, 0, a.total_q), end = packed_offset(a.offsets_q, a.sequences, a.total_q);
+    float m = -__builtin_inff(), l = 0.f, w[E];
+    bool any[E];
 #pragma unroll
-        for (int e = 0; e < N; e++) v[e] = o[(size_t)p * D + e];
-#pragma unroll
-        for (int e = 0; e < N; e++) x[e] = with_keys >> p & 1 ? fmaf(v[e], wp, x[e]) : x[e];
+    for (int i = 0; i < E; i++) {
+        any[i] = f + i * G < parts && e[i][1] != 0.f;      // (a part without keys for this row: its accumulators were not written)
+        m = fmaxf(m, any[i] ? e[i][0] : -__builtin_inff());
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    T* op = reinterpret_cast<T*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head) + lane * N;
 #pragma unroll
-    for (int e = 0; e < N; e++) op[e] = from_f32<T>(x[e] * inv);
+    for (int s = G / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+#pragma unroll
+    for (int i = 0; i < E; i++) {
+        w[i] = !any[i] ? -1.f : e[i][0] == m ? 1.f : __builtin_amdgcn_exp2f((e[i][0] - m) * c);
+        l += any[i] ? e[i][1] * w[i] : 0.f;
+    }
+#pragma unroll
+    for (int s = G / 2; s > 0; s >>= 1) l += __shfl_xor(l, s, 64);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < E; i++) {
+        for (int p0 = i * G; p0 < min((i + 1) * G, parts); p0 += U) {
+            f32x4 v[U];
+#pragma unroll
+            for (int j = 0; j < U; j++) v[j] = *reinterpret_cast<const f32x4*>(o + (size_t)min(p0 + j, parts - 1) * D);
+#pragma unroll
+            for (int j = 0; j < U; j++) {
+                const float wp = p0 + j < parts ? __shfl(w[i], g * G + p0 + j - i * G, 64) : -1.f;
+#pragma unroll
+                for (int k = 0; k < 4; k++) x[k] = wp >= 0.f ? fmaf(v[j][k], wp, x[k]) : x[k];
+            }
+        }
+    }
+    const int tok = packed_div((int)r, by_q_heads), head = (int)r - tok * a.q_heads;
+    if (row >= all || tok < begin || tok >= end) return;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    *reinterpret_cast<tx4*>(static_cast<char*>(a.o) + (size_t)tok * a.o_token + (size_t)head * a.o_head + 4 * f * sizeof(T)) =
+        tx4{from_f32<T>(x[0] * inv), from_f32<T>(x[1] * inv), from_f32<T>(x[2] * inv), from_f32<T>(x[3] * inv)};
 }
 
 template <typename T, int D>
 int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
-    PackedAttnArgs m = a;
-    m.parts = 1;
-    m.blocks = (int)packed_blocks(a, kPackedRowsMerge);
+    constexpr size_t kRows = 4 * (64 / (D / 4));         // of a workgroup
     HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
-    const dim3 grid = packed_grid(m);
-    hipLaunchKernelGGL((packed_merge_kernel<T, D>), grid, dim3(256), 0, st, m, a.parts, sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid_of(((size_t)a.total_q * a.q_heads + kRows - 1) / kRows), dim3(256), 0, st, a, packed_divisor((unsigned)a.q_heads),
+                       sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
     return hyb_check_launch("packed_attention_merge");
 }
 
 // How many parts the keys of a block are cut into; each block deals its own keys out to them.  The least over an estimate of a launch's length in us: the longest part's keys at the pace of a
 // workgroup that is alone on its CU, or all blocks' at the pace of a full chip, whatever is longer; the start of the workgroups; the merge: a launch, a share per row, the partial results that are
-// written and read.  Fitted to 302 launches of 1 to 64 sequences of 50 to 9000 keys, in caches and out of them, each in 1 to 32 parts: 1 % above the best on average, 3 % where the keys come from
+// written and read.  Fitted to 344 launches of 1 to 64 sequences of 50 to 9000 keys, in caches and out of them, each in 1 to 32 parts: 1.4 % above the best on average, 3 % where the keys come from
 // memory (as many parts as fill the chip: 7 and 9 %; 10 heads of 64, 8 sequences of 648: not cut 21 us, in two 43; 17 tokens over 2031 to 3695 keys, 16 / 8 heads of 128: 69 and, in six, 22).
 // Never more than the chip holds at once.  max_k == 0: half as many again as the mean; it decides the number of parts only.
 void choose_parts(PackedAttnArgs& a, int max_k, bool f32, int head_dim) {
@@ -299,11 +314,12 @@ void choose_parts(PackedAttnArgs& a, int max_k, bool f32, int head_dim) {
     const double blocks = ((double)a.total_q * a.group / (f32 ? packed_rows_f32(head_dim) : kPackedRowsMfma) + 0.5 * a.sequences) * a.k_heads;
     const double seen = a.causal && a.total_q == a.total_k ? 0.5 * mean : mean, all = blocks * seen * key / (hyb_cu_count() * (f32 ? 1.2 : 1.6));
     const double rows = (double)a.total_q * a.q_heads;
+    if (rows > 1 << 30) return;                     // (the merge counts rows in 32 bits)
     double best = 0;
     const int slots = hyb_cu_count() * (f32 ? 2 : head_dim == 64 ? 4 : 3);
     for (int parts = 1; parts <= kPackedMaxParts && (parts == 1 || ((parts - 1) * kPackedPartKeys < keys && parts * blocks <= slots)); parts++) {
         const double share = keys / parts > kPackedPartKeys ? keys / parts : kPackedPartKeys, own = (parts == 1 ? keys : share) * key;
-        const double merge = parts == 1 ? 0 : 2.4 + rows * (0.2e-3 + 0.1e-3 * parts * head_dim / 64);
+        const double merge = parts == 1 ? 0 : 2.4 + rows * (0.1e-3 + 0.1e-3 * parts * head_dim / 64);
         const double us = (own > all ? own : all) + 0.003 * blocks * parts + merge;
         if (parts == 1 || us < best) {
             best = us;
