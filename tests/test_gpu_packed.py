@@ -312,6 +312,23 @@ def test_attention_cut_keys_without_hints(hb, dt, d):
     _check(dt, *got)
 
 
+@pytest.mark.parametrize("dt,hint", [("bf16", 1), ("bf16", 0), ("f32", 0)])
+def test_attention_more_workgroups_than_one_grid_dimension_holds(hb, dt, hint):
+    """300000 sequences of one query and one key, 32 heads: 9.6 million units.  The one probability is 1, so o is v but for the rounding of p v / p: none in bf16 (the products of two
+    8-bit significands are exact, the quotient is off by 2^-23 at most, far inside half a step), three of 2^-24 in fp32."""
+    n = 300000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = (torch.randn(n, 32, 64, generator=g, device="cuda").to(tdt(dt)) for _ in range(3))
+    o = torch.full_like(q, 7.0)
+    cu = torch.arange(n + 1, device="cuda", dtype=torch.int32)
+    desc = hb.packed_attention_desc(q, k, v, o, cu, hint, hint)
+    hb.hyb_packed_attention(desc, q, k, v, o, cu, cu, torch.empty(max(hb.hyb_packed_attention_workspace_bytes(desc), 16), device="cuda", dtype=torch.uint8))
+    if dt == "bf16":
+        assert torch.equal(o, v)
+    else:
+        assert bool(((o - v).abs() <= 3 * 2.0 ** -24 * v.abs()).all())
+
+
 @pytest.mark.parametrize("hints", [False, 1, 600, 100000])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_hints_do_not_decide_the_result(hb, dt, hints):
