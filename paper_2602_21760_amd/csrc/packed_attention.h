@@ -28,6 +28,7 @@ struct PackedAttnArgs {
     float scale;                                  // > 0; PRE kernels do not use it
     int causal, prescaled;
     size_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in bytes
+    int rows;                                     // rows of a block (few-rows kernel: not used)
     int blocks;                                   // row blocks of all sequences, an upper bound (see packed_find)
     int parts;                                    // the keys of a block are cut into up to `parts` parts (see packed_part_tiles); 1: not cut
     int pieces, part_keys;                        // few-rows kernel: pieces of part_keys keys of all sequences, an upper bound; 0 otherwise
@@ -56,7 +57,6 @@ constexpr int kPackedRowsFew = 16;                                              
 constexpr int kPackedMaxParts = 64;
 constexpr int kPackedPartKeys = 256;                                                 // least keys of a part
 constexpr int packed_tile_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }    // keys of its LDS tiles
-constexpr int packed_rows_f32(int head_dim) { return head_dim == 64 ? 32 : 16; }     // fp32
 
 // Most blocks of `rows` rows that any offsets can ask for.
 inline long long packed_blocks(const PackedAttnArgs& a, int rows) { return (long long)a.total_q * a.group / rows + a.sequences; }

@@ -1,15 +1,16 @@
 // fp32 attention over packed batches on the fp32 matrix cores (reference precision), the merge of cut keys for both types, and the entry point.
 //
-// As attention_f32.hip: a workgroup of 4 waves owns 32 rows (head_dim 128: 16) of one (sequence, key head) and splits the KEYS: wave w takes the 32-key
-// tiles w, w + 4, ... with a running reference and normaliser of its own; the four partial results are merged in LDS in a fixed order.  Operands go
-// straight from memory (L2) to registers.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: a 16-byte load gives a lane 4 features of its key
-// for 4 MFMAs, and register i of the exponentiated S^T is the B operand of the MFMA over the keys 4 q4 + i, with rows 4 q4 + i of V as the A operand.
+// A workgroup of 4 waves owns 32 rows (small launches at head_dim 128: 16) of one (sequence, key head) and splits the KEYS: wave w takes the 32-key tiles w, w + 4, ... with a running reference and normaliser of
+// its own; the four partial results are merged in LDS in a fixed order.  Keys and values go straight from memory (L2) to registers, the queries, which all waves share, lie in LDS.
+// S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: a 16-byte load gives a lane 4 features of its key for 4 MFMAs, and register i of the exponentiated S^T is the B operand of
+// the MFMA over the keys 4 q4 + i, with rows 4 q4 + i of V as the A operand.
 //
-// Bound by the matrix cores, which share their issue with everything else here: fp32 MFMAs and vector instructions of the two waves of a SIMD do not overlap (busy 63 % and 24 % of the time
+// Bound by the matrix cores, which share their issue with everything else here: fp32 MFMAs and vector instructions of the waves of a SIMD do not overlap (busy 63 % and 24 % of the time
 // with 382 vector instructions beside the 128 MFMAs of a tile, no better with waves of different priority).  So a tile has few others: a probability is one fma and one
 // v_exp_f32, 2^(c score - reference), whose error is that of an argument near 0 wherever the probability counts; masks, maxima across lanes and rescaling only where a tile asks for them;
-// offsets of buffer loads that no tile changes.  One sequence of 4096, 8 heads: head_dim 64 127 TFLOP/s, 128 107 (a large library product in fp32 reaches 139); 16 rows at head_dim 64 110.
-// Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles and by the last round (314, 1302 and 259 tokens, 12 / 4 heads of 64: 57 to 65 us from card to card, 88 to 100 TFLOP/s).
+// offsets of buffer loads that no tile changes.  One sequence of 4096, 8 heads: head_dim 64 130 TFLOP/s, 128 118 (a large library product in fp32 reaches 139); with 16 rows 110 and 107.
+// The queries in LDS make room for a third workgroup at head_dim 64 (in registers, with the next tile's keys requested ahead: 314, 1302 and 259 tokens, 12 / 4 heads, 65 us, so 61) and for
+// 32 rows at 128 (16 rows: 800, 300 and 1200 tokens, causal, 16 / 8 heads, 115 us, so 99; three sequences of 142 to 605, 4 heads: 25 and 34).  Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles.
 #include "packed_attention.h"
 
 namespace {
@@ -20,9 +21,9 @@ constexpr float RESCALE_LOG2 = 8.0f;
 
 __device__ __forceinline__ f32x4 load16(__amdgpu_buffer_rsrc_t rsrc, int offset) { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0)); }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
-    constexpr int BQ = packed_rows_f32(D), QT = BQ / 16, DT = D / 16, VH = D / 64;
+template <int D, int BQ>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
+    constexpr int QT = BQ / 16, DT = D / 16, VH = D / 64;
     __shared__ float part_o[WAVES][QT][DT][4][64];   // [wave][row tile][feature tile][register][lane]
     __shared__ float part_ml[WAVES][QT][2][16];      // [wave][row tile][maximum, normaliser][row]
     const PackedUnit u = packed_unit<BQ, true>(a, packed_group_id());
@@ -33,16 +34,18 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
     const char* vp = static_cast<const char*>(a.v) + (size_t)u.k0 * a.v_token + (size_t)u.head * a.v_head;
 
     const float c = a.prescaled ? 1.f : a.scale * 1.4426950408889634f;
-    f32x4 q[QT][DT];     // [row tile][16-feature step]
     int last[QT];
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        const int row = u.row0 + min(qt * 16 + l16, u.rows - 1), t = packed_div(row, a.by_group);
-        last[qt] = packed_last_key(a, u, t);
-        const char* qp = static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + row - t * a.group) * a.q_head;
+    for (int qt = 0; qt < QT; qt++) last[qt] = packed_last_key(a, u, packed_div(u.row0 + min(qt * 16 + l16, u.rows - 1), a.by_group));
+    // the queries in LDS, where the waves' results go later: 16-byte slot s of row r at s ^ (r % 16)
+    f32x4* const q = reinterpret_cast<f32x4*>(&part_o[0][0][0][0][0]);
 #pragma unroll
-        for (int s = 0; s < DT; s++) q[qt][s] = *reinterpret_cast<const f32x4*>(qp + 64 * s + 16 * q4);
+    for (int i = 0; i < BQ * D / 4 / 256; i++) {
+        const int r = (threadIdx.x + 256 * i) / (D / 4), slot = threadIdx.x % (D / 4), row = u.row0 + min(r, u.rows - 1), t = packed_div(row, a.by_group);
+        q[r * (D / 4) + (slot ^ (r % 16))] =
+            *reinterpret_cast<const f32x4*>(static_cast<const char*>(a.q) + (size_t)(u.q0 + t) * a.q_token + (size_t)(u.head * a.group + row - t * a.group) * a.q_head + 16 * slot);
     }
+    __syncthreads();
     const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group)), block_max = packed_last_key(a, u, packed_div(u.row0 + u.rows - 1, a.by_group));
     const int nt = (block_max + BKV) / BKV, part_tiles = packed_part_tiles(a, nt, BKV);
     const int t_begin = min(u.part * part_tiles, nt), t_end = min(t_begin + part_tiles, nt);
@@ -64,43 +67,41 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
 #pragma unroll
         for (int i = 0; i < 4; i++) v_off[kt][i] = (kt * 16 + 4 * q4 + i) * (int)a.v_token + 16 * l16;
     }
-    f32x4 k[2][DT];      // [key tile][16-feature step]
-    auto load_k = [&](int t) {
-        const int key0 = t * BKV, more = min(u.n_k - key0, BKV) - 1;
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)key0 * a.k_token), 0, more * (int)a.k_token + 4 * D, 0x00020000);
-#pragma unroll
-        for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-            for (int s = 0; s < DT; s++) k[kt][s] = load16(rsrc, k_off[kt] + 64 * s);
-    };
-    // head_dim 64: the next tile's keys are requested as soon as this one's scores stand (one sequence of 4096, 8 heads: 277 us without, 271 so; at 128 it takes registers that are not there)
-    constexpr bool AHEAD = D == 64;
-    if (AHEAD && t_begin + wave < t_end) load_k(t_begin + wave);
     for (int t = t_begin + wave; t < t_end; t += WAVES) {
         const int key0 = t * BKV, more = min(u.n_k - key0, BKV) - 1;
+        const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)key0 * a.k_token), 0, more * (int)a.k_token + 4 * D, 0x00020000);
         const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + (size_t)key0 * a.v_token), 0, more * (int)a.v_token + 4 * D, 0x00020000);
-        f32x4 v[2][4][VH];   // [key tile][row 4 q4 + i][64 features]
-        if constexpr (!AHEAD) load_k(t);
+        f32x4 k[2][DT], v[2][4][VH];     // K: [key tile][16-feature step]; V: [key tile][row 4 q4 + i][64 features]
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+            for (int s = 0; s < DT; s++) k[kt][s] = load16(k_rsrc, k_off[kt] + 64 * s);
+        auto load_v = [&](int kt) {
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int h = 0; h < VH; h++) v[kt][i][h] = load16(v_rsrc, v_off[kt][i] + 256 * h);
+        };
+        load_v(0);
+        if constexpr (D == 64 || BQ == 16) load_v(1);
         f32x4 s[2][QT];      // [key tile][row tile]: keys 16 kt + 4 q4 + i
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
             for (int qt = 0; qt < QT; qt++) s[kt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < DT; st++)
+        for (int st = 0; st < DT; st++) {
+            f32x4 qs[QT];
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) qs[qt] = q[(qt * 16 + l16) * (D / 4) + ((4 * st + q4) ^ l16)];
 #pragma unroll
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-                    for (int qt = 0; qt < QT; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][st][j], q[qt][st][j], s[kt][qt], 0, 0, 0);
-        if constexpr (AHEAD) load_k(min(t + WAVES, t_end - 1));      // (the last one again: with a branch, the wait for the values would be one for these)
+                    for (int qt = 0; qt < QT; qt++) s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][st][j], qs[qt][j], s[kt][qt], 0, 0, 0);
+        }
+        if constexpr (D == 128 && BQ == 32) load_v(1);       // (into registers that the keys leave)
         const bool masked = key0 + BKV - 1 > block_min;
         if (masked) {
 #pragma unroll
@@ -162,6 +163,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
                     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
                         for (int i = 0; i < 4; i++) {
+                            __builtin_amdgcn_sched_barrier(0);      // (one value at a time: this path's registers count for the whole kernel)
                             unsigned x = *reinterpret_cast<const unsigned*>(vp + (size_t)key * a.v_token + 4 * ((dt / 4) * 64 + 16 * q4 + 4 * i + dt % 4));
                             x &= odd_mask_f32(x);
 #pragma unroll
@@ -188,6 +190,7 @@ __global__ __launch_bounds__(256, 2) void packed_attention_f32_kernel(PackedAttn
                     for (int qt = 0; qt < QT; qt++) o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[kt][i][dt / 4][dt % 4], s[kt][qt][i], o[dt][qt], 0, 0, 0);
     }
 
+    __syncthreads();         // everyone is done with the queries
     // merge of the waves: row = sum_p o_p 2^(m_p - M) / sum_p l_p 2^(m_p - M), p in order
 #pragma unroll
     for (int qt = 0; qt < QT; qt++) {
@@ -311,7 +314,7 @@ void choose_parts(PackedAttnArgs& a, int max_k, bool f32, int head_dim) {
     const double mean = (double)a.total_k / a.sequences, most = max_k > 0 ? max_k : 1.5 * mean, keys = most < a.total_k ? most : a.total_k;
     if (!f32 && keys <= 512) return;                // (bf16 blocks of so few keys gain nothing: 10.5 us, cut 12.9)
     const double key = f32 ? (head_dim == 64 ? 0.015 : 0.025) : head_dim == 64 ? 0.009 : 0.014;
-    const double blocks = ((double)a.total_q * a.group / (f32 ? packed_rows_f32(head_dim) : kPackedRowsMfma) + 0.5 * a.sequences) * a.k_heads;
+    const double blocks = ((double)a.total_q * a.group / a.rows + 0.5 * a.sequences) * a.k_heads;
     const double seen = a.causal && a.total_q == a.total_k ? 0.5 * mean : mean, all = blocks * seen * key / (hyb_cu_count() * (f32 ? 1.2 : 1.6));
     const double rows = (double)a.total_q * a.q_heads;
     if (rows > 1 << 30) return;                     // (the merge counts rows in 32 bits)
@@ -378,7 +381,10 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     if (d.dtype == HYB_BF16 && d.max_q > 0 && (long long)d.max_q * a.group <= kPackedRowsFew) {
         choose_pieces(a, d.max_k, hyb_cu_count() * (d.head_dim == 64 ? 4 : 2));
     } else {
-        a.blocks = (int)packed_blocks(a, d.dtype == HYB_BF16 ? kPackedRowsMfma : packed_rows_f32(d.head_dim));
+        // fp32, head_dim 128: blocks of 32 rows where they fill three quarters of the chip's two workgroups a CU, of 16 otherwise
+        const bool small = d.head_dim == 128 && ((long long)d.total_q * a.group / 32 + d.sequences / 2) * a.k_heads * 2 < 3 * hyb_cu_count();
+        a.rows = d.dtype == HYB_BF16 ? kPackedRowsMfma : small ? 16 : 32;
+        a.blocks = (int)packed_blocks(a, a.rows);
         if (d.sequences > 0) choose_parts(a, d.max_k, d.dtype == HYB_F32, d.head_dim);
     }
     return HYB_OK;
@@ -394,8 +400,9 @@ size_t scratch_bytes(const PackedAttnArgs& a, int head_dim) {
 int hyb_launch_packed_attention_f32(PackedAttnArgs& a, int head_dim, hipStream_t st) {
     const dim3 grid = packed_grid(a);
     HybTraceScope trace("packed_attention_f32", "byte", 8.0 * head_dim * ((double)a.total_q * a.q_heads + (double)a.total_k * a.k_heads), st);
-    if (head_dim == 64) hipLaunchKernelGGL(packed_attention_f32_kernel<64>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(packed_attention_f32_kernel<128>, grid, dim3(256), 0, st, a);
+    if (head_dim == 64) hipLaunchKernelGGL((packed_attention_f32_kernel<64, 32>), grid, dim3(256), 0, st, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((packed_attention_f32_kernel<128, 32>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((packed_attention_f32_kernel<128, 16>), grid, dim3(256), 0, st, a);
     return hyb_check_launch("packed_attention_f32");
 }
 
