@@ -413,6 +413,35 @@ def test_attention_hidden_keys_do_not_reach_few_queries(hb, dt, d, bad):
     assert np.isfinite(got[~dirty]).all() and (np.abs(got - clean)[~dirty] <= bound[~dirty]).all()
 
 
+@pytest.mark.parametrize("prescaled", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_f32_launches_that_fill_the_chip(hb, causal, prescaled):
+    """Blocks of 32 rows at head_dim 128."""
+    lens = [130, 70, 0, 33, 1, 97]
+    _check("f32", *_attention(hb, "f32", lens, lens if causal else [64, 131, 9, 33, 1, 200], 64, 32, 128, causal=causal, prescaled=prescaled, spare=2, layout="kv"))
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_attention_f32_launches_that_fill_the_chip_hidden_keys(hb, bad):
+    lens = [130, 70, 0, 33, 1, 97]
+
+    def edit(q, k, v, cu_q, cu_k):
+        for x in (k, v):
+            x[:2] = bad
+            x[cu_k[-1]:] = bad
+        v[cu_k[1] - 1, :, 7] = bad                         # the last key of the first sequence, seen by its last query
+        v[cu_k[1] + 40, 3] = bad
+    got, want, inputs, same, _ = _attention(hb, "f32", lens, lens, 64, 32, 128, causal=True, spare=2, edit=edit, layout="kv")
+    q, k, v, cu_q, cu_k, causal, factor = inputs
+    dirty = np.zeros(got.shape, dtype=bool)
+    dirty[cu_q[1] - 1, :, 7] = True
+    dirty[cu_q[1] + 40:cu_q[2], 6:8] = True
+    assert same and not np.isfinite(got[dirty]).any() and np.isfinite(got[~dirty]).all()
+    k, v = (np.where(np.isfinite(x), x, 0.0) for x in (k, v))
+    clean = P.packed_attention(q, k, v, cu_q, cu_k, causal, factor, np.full(got.shape, 7.0))
+    assert (np.abs(got - clean)[~dirty] <= P.packed_attention_bound(q, k, v, cu_q, cu_k, False, causal, factor)[~dirty]).all()
+
+
 @pytest.mark.parametrize("new", [0, 2])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
