@@ -333,15 +333,17 @@ void choose_parts(PackedAttnArgs& a, int max_k, bool f32, int head_dim) {
 
 // Pieces of the few-rows kernel: all keys dealt out over the chip, two pieces for every workgroup that fits it (one: 11 % slower over caches of 100 to 8000 keys, three: the same), of at
 // least 256 keys (8000 keys of one sequence, 8 heads of 128: 11.7 us; of 512: 13.0), or 512 where the sequences alone fill the chip.  Sequences of which the caller says that none is
-// longer than a piece are one piece each, whatever their length, and need no join.  So are those of up to 2048 keys and much the same length that keep a third of the chip busy: what
-// pieces cost in starts and join is more than what they even out (8 heads of 128: 40 caches of 630 to 700 keys 24.8 us, in pieces 31.0; 87 of 1080 to 1200 77 / 97; 53 of 1800 to 2000
-// 82 / 93; of 2700 to 3000 125 / 132, but 40 of them 110 / 103.  256 caches of which every second has 2000 keys, the others 50, 4 heads: 130 / 118).
-void choose_pieces(PackedAttnArgs& a, int max_k, int slots) {
+// longer than a piece are one piece each, whatever their length, and need no join.  So are those of up to 1024 keys (head_dim 128: 768; the join costs more than they take: 16 caches of up to 600, 32 / 8
+// heads of 64, 11.3 us, so 8.3; one of 1024 9.7 both, of 2000 9.7 and 13.9), and those of up to 2048 and much the same length that keep a quarter of the CUs busy: what pieces cost in starts
+// and join is more than what they even out (8 heads of 128: 40 caches of 630 to 700 keys 24.8 us, in pieces 31.0; 87 of 1080 to 1200 77 / 97; 16 of up to 2000 22.3 / 24.6; 4 of up to 2000 19.1 / 13.4;
+// 53 of 2700 to 3000 125 / 132, but 40 of them 110 / 103.  256 caches of which every second has 2000 keys, the others 50, 4 heads: 130 / 118).
+void choose_pieces(PackedAttnArgs& a, int max_k, int head_dim) {
+    const int slots = hyb_cu_count() * (head_dim == 64 ? 4 : 2);
     long long len = ((long long)a.total_k * a.k_heads / (2 * slots) + 63) / 64 * 64;
     const int least = (long long)a.sequences * a.k_heads >= slots ? 512 : 256;
     if (len < least) len = least;
-    const bool alike = max_k <= 2048 && 4ll * a.sequences * max_k <= 7ll * a.total_k && 3ll * a.total_k * a.k_heads >= (long long)max_k * slots;
-    if (max_k > 0 && (max_k <= len || alike)) len = 1 << 30;
+    const bool alike = max_k <= 2048 && 4ll * a.sequences * max_k <= 7ll * a.total_k && 4ll * a.total_k * a.k_heads >= (long long)max_k * hyb_cu_count();
+    if (max_k > 0 && (max_k <= len || max_k <= (head_dim == 64 ? 1024 : 768) || alike)) len = 1 << 30;
     a.part_keys = (int)len;
     a.by_piece = packed_divisor((unsigned)len);
     a.pieces = (int)(a.total_k / len) + a.sequences;
@@ -379,7 +381,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     a.parts = 1;
     // at most 16 rows per sequence: the kernel whose waves split the keys (only the sizes that the caller names can say so; any others are right, too)
     if (d.dtype == HYB_BF16 && d.max_q > 0 && (long long)d.max_q * a.group <= kPackedRowsFew) {
-        choose_pieces(a, d.max_k, hyb_cu_count() * (d.head_dim == 64 ? 4 : 2));
+        choose_pieces(a, d.max_k, d.head_dim);
     } else {
         // fp32, head_dim 128: blocks of 32 rows where they fill three quarters of the chip's two workgroups a CU, of 16 otherwise
         const bool small = d.head_dim == 128 && ((long long)d.total_q * a.group / 32 + d.sequences / 2) * a.k_heads * 2 < 3 * hyb_cu_count();
