@@ -679,6 +679,39 @@ def test_packed_block_replays_from_a_graph(hb):
     assert err(host(replayed), oracle(MIXED)) < tol("bf16")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt,new", [("bf16", 1), ("bf16", 20), ("f32", 1), ("f32", 20)])
+def test_cut_keys_replay_from_a_graph(hb, dt, new, d):
+    """Both launches of a call whose keys are cut, captured once: replays follow the offsets, whatever the workspace holds, and give the bits of an eager call."""
+    n, rows = 5, 6000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.randn(n * new, 4, d, generator=g, device="cuda").to(tdt(dt))
+    k, v = (torch.randn(rows, 2, d, generator=g, device="cuda").to(tdt(dt)) for _ in range(2))
+    o, cu_q = torch.empty_like(q), _offsets([new] * n)
+    cu_k = torch.empty(n + 1, dtype=torch.int32, device="cuda")
+    desc = hb.packed_attention_desc(q, k, v, o, cu_q, new, 4000, causal=True)
+    need = hb.hyb_packed_attention_workspace_bytes(desc)
+    assert need > 0
+    ws, own = (torch.empty(need, device="cuda", dtype=torch.uint8) for _ in range(2))
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    cu_k.copy_(_offsets([1200] * n))
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        hb.hyb_packed_attention(desc, q, k, v, o, cu_q, cu_k, ws)
+    for lens in ([1200] * 5, [4000, 0, 500, 1, 1499], [30, 40, 3000, 2000, 25], [1200] * 5):
+        cu_k.copy_(_offsets(lens))
+        ws.fill_(255)
+        o.fill_(7.0)
+        graph.replay()
+        eager = torch.full_like(o, 7.0)
+        own.fill_(255)
+        hb.hyb_packed_attention(desc, q, k, v, eager, cu_q, cu_k, own)
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager), lens
+        args = host(q), host(k), host(v), cu_q.cpu().numpy(), cu_k.cpu().numpy()
+        assert (np.abs(host(o) - P.packed_attention(*args, True)) <= P.packed_attention_bound(*args, dt == "bf16", True)).all(), lens
+
+
 def test_two_streams_with_a_workspace_each(hb):
     """Calls that overlap in time, on streams of their own."""
     lk = [3000, 1700]
