@@ -24,7 +24,7 @@ __device__ __forceinline__ f32x4 load16(__amdgpu_buffer_rsrc_t rsrc, int offset)
 template <int D, int BQ>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_attention_f32_kernel(PackedAttnArgs a) {
     constexpr int QT = BQ / 16, DT = D / 16, VH = D / 64;
-    __shared__ float part_o[WAVES][QT][DT][4][64];   // [wave][row tile][feature tile][register][lane]
+    __shared__ f32x4 part_o[WAVES][QT][DT][64];      // [wave][row tile][feature tile][lane]
     __shared__ float part_ml[WAVES][QT][2][16];      // [wave][row tile][maximum, normaliser][row]
     const PackedUnit u = packed_unit<BQ, true>(a, packed_group_id());
     if (u.rows == 0) return;
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_attention_f32_ker
 #pragma unroll
     for (int qt = 0; qt < QT; qt++) last[qt] = packed_last_key(a, u, packed_div(u.row0 + min(qt * 16 + l16, u.rows - 1), a.by_group));
     // the queries in LDS, where the waves' results go later: 16-byte slot s of row r at s ^ (r % 16)
-    f32x4* const q = reinterpret_cast<f32x4*>(&part_o[0][0][0][0][0]);
+    f32x4* const q = &part_o[0][0][0][0];
 #pragma unroll
     for (int i = 0; i < BQ * D / 4 / 256; i++) {
         const int r = (threadIdx.x + 256 * i) / (D / 4), slot = threadIdx.x % (D / 4), row = u.row0 + min(r, u.rows - 1), t = packed_div(row, a.by_group);
@@ -201,45 +201,45 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_attention_f32_ker
             part_ml[wave][qt][1][l16] = l[qt];
         }
 #pragma unroll
-        for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) part_o[wave][qt][dt][i][lane] = o[dt][qt][i];
+        for (int dt = 0; dt < DT; dt++) part_o[wave][qt][dt][lane] = o[dt][qt];
     }
     __syncthreads();
-    // wave w finishes register w of every tile: features 64 h + 16 q4 + 4 w .. + 3 of row l16
+    // a wave finishes one row tile's 64 features, or half of their registers: register i of feature tiles 4 h .. 4 h + 3 is features 64 h + 16 q4 + 4 i .. + 3 of row l16
+    constexpr int SPLIT = WAVES / (QT * VH), NI = 4 / SPLIT;
+    typedef float regs __attribute__((ext_vector_type(NI)));
+    const int qt = wave / SPLIT / VH, h = wave / SPLIT % VH, i0 = wave % SPLIT * NI;
+    if (qt * 16 + l16 >= u.rows) return;
+    float m_all = part_ml[0][qt][0][l16], l_all = 0.f;
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        if (qt * 16 + l16 >= u.rows) continue;
-        float m_all = part_ml[0][qt][0][l16];
+    for (int p = 1; p < WAVES; p++) m_all = fmaxf(m_all, part_ml[p][qt][0][l16]);
+    f32x4 r[NI];
 #pragma unroll
-        for (int p = 1; p < WAVES; p++) m_all = fmaxf(m_all, part_ml[p][qt][0][l16]);
-        float l_all = 0.f;
-        f32x4 r[VH];
+    for (int i = 0; i < NI; i++) r[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < VH; h++) r[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < WAVES; p++) {
+        const float mp = part_ml[p][qt][0][l16], lp = part_ml[p][qt][1][l16];
+        if (lp == 0.f) continue;     // a wave without keys for this row counts nothing
+        const float w = mp == m_all ? 1.f : __builtin_amdgcn_exp2f(mp - m_all);
+        l_all = fmaf(lp, w, l_all);
 #pragma unroll
-        for (int p = 0; p < WAVES; p++) {
-            const float mp = part_ml[p][qt][0][l16], lp = part_ml[p][qt][1][l16];
-            if (lp == 0.f) continue;     // a wave without keys for this row counts nothing
-            const float w = mp == m_all ? 1.f : __builtin_amdgcn_exp2f(mp - m_all);
-            l_all = fmaf(lp, w, l_all);
+        for (int e = 0; e < 4; e++) {
+            const regs y = *reinterpret_cast<const regs*>(reinterpret_cast<const float*>(&part_o[p][qt][4 * h + e][lane]) + i0);
 #pragma unroll
-            for (int h = 0; h < VH; h++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) r[h][e] = fmaf(part_o[p][qt][4 * h + e][wave][lane], w, r[h][e]);
+            for (int i = 0; i < NI; i++) r[i][e] = fmaf(y[i], w, r[i][e]);
         }
-        const int row = u.row0 + qt * 16 + l16, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
-        if (a.parts > 1) {
-            const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
-            if (q4 == 0 && wave == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{m_all, l_all};
-#pragma unroll
-            for (int h = 0; h < VH; h++) *reinterpret_cast<f32x4*>(a.part + at * D + 64 * h + 16 * q4 + 4 * wave) = r[h];
-            continue;
-        }
-        char* op = static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head + 4 * (16 * q4 + 4 * wave);
-#pragma unroll
-        for (int h = 0; h < VH; h++) *reinterpret_cast<f32x4*>(op + 256 * h) = l_all == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : r[h] / l_all;
     }
+    const int row = u.row0 + qt * 16 + l16, tok = packed_div(row, a.by_group), head = u.head * a.group + (row - tok * a.group);
+    const int feature = 64 * h + 16 * q4 + 4 * i0;
+    if (a.parts > 1) {
+        const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
+        if (feature == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{m_all, l_all};
+#pragma unroll
+        for (int i = 0; i < NI; i++) *reinterpret_cast<f32x4*>(a.part + at * D + feature + 4 * i) = r[i];
+        return;
+    }
+    float* op = reinterpret_cast<float*>(static_cast<char*>(a.o) + (size_t)(u.q0 + tok) * a.o_token + (size_t)head * a.o_head) + feature;
+#pragma unroll
+    for (int i = 0; i < NI; i++) *reinterpret_cast<f32x4*>(op + 4 * i) = l_all == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : r[i] / l_all;
 }
 
 // Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
