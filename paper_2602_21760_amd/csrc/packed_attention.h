@@ -40,7 +40,7 @@ struct PackedAttnArgs {
     PackedDivisor by_heads, by_parts;             // heads of an XCD, parts
 };
 
-// Scratch of cut keys.  Blocks of rows that are cut (all but the few-rows kernel): for each (row of q, head) `parts` unnormalised accumulators of head_dim values, then for each `parts` pairs (reference, sum).
+// Scratch of cut keys.  Blocks of rows that are cut (all but the few-rows kernel): for each (row of q, head) `parts` unnormalised accumulators of head_dim values, then for each `parts` pairs (reference in base 2, sum).
 __host__ __device__ inline size_t packed_part_floats(int total_q, int q_heads, int parts, int head_dim) {
     return (size_t)total_q * q_heads * parts * (head_dim + 2);
 }

@@ -242,12 +242,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_attention_f32_ker
     for (int i = 0; i < NI; i++) *reinterpret_cast<f32x4*>(op + 4 * i) = l_all == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : r[i] / l_all;
 }
 
-// Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^((m_p - M) c)
-// (fp32: references are in base 2, c = 1), M = max m_p over the parts with keys, parts in index order.  D / 4 lanes per row, four features each; lane f has the weights of parts f, f + D / 4, ...
+// Joins the parts of cut keys: with references m_p, normalisers l_p and accumulators o_p a row is sum_p o_p w_p / sum_p l_p w_p, w_p = 2^(m_p - M),
+// M = max m_p over the parts with keys, parts in index order.  D / 4 lanes per row, four features each; lane f has the weights of parts f, f + D / 4, ...
 // Rows are those of all offsets (they do not decrease), so no sequence has to be found: one trip to memory for the pairs and the first accumulators, one for every eight more.  Bound
 // by that latency and, for many rows, by the partial results it reads.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, PackedDivisor by_q_heads, float c) {
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, PackedDivisor by_q_heads) {
     constexpr int G = D / 4, ROWS = 64 / G, E = kPackedMaxParts / G, U = 8;
     typedef T tx4 __attribute__((ext_vector_type(4)));
     const int lane = threadIdx.x % 64, g = lane / G, f = lane % G, parts = a.parts;
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedAttnArgs a, Pac
     for (int s = G / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
 #pragma unroll
     for (int i = 0; i < E; i++) {
-        w[i] = !any[i] ? -1.f : e[i][0] == m ? 1.f : __builtin_amdgcn_exp2f((e[i][0] - m) * c);
+        w[i] = !any[i] ? -1.f : e[i][0] == m ? 1.f : __builtin_amdgcn_exp2f(e[i][0] - m);
         l += any[i] ? e[i][1] * w[i] : 0.f;
     }
 #pragma unroll
@@ -300,8 +300,7 @@ template <typename T, int D>
 int launch_merge(const PackedAttnArgs& a, hipStream_t st) {
     constexpr size_t kRows = 4 * (64 / (D / 4));         // of a workgroup
     HybTraceScope trace("packed_attention_merge", "byte", 4.0 * packed_part_floats(a.total_q, a.q_heads, a.parts, D), st);
-    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid_of(((size_t)a.total_q * a.q_heads + kRows - 1) / kRows), dim3(256), 0, st, a, packed_divisor((unsigned)a.q_heads),
-                       sizeof(T) == 4 || a.prescaled ? 1.f : a.scale * 1.4426950408889634f);
+    hipLaunchKernelGGL((packed_merge_kernel<T, D>), packed_grid_of(((size_t)a.total_q * a.q_heads + kRows - 1) / kRows), dim3(256), 0, st, a, packed_divisor((unsigned)a.q_heads));
     return hyb_check_launch("packed_attention_merge");
 }
 

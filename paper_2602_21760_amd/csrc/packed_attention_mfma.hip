@@ -424,10 +424,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
         if (a.parts > 1) {
             if (wave * 32 + qt * 16 + l16e >= u.rows) continue;
             const size_t at = ((size_t)(u.q0 + tok) * a.q_heads + head) * a.parts + u.part;
-            if (q4e == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : m_run[qt], l};
+            // references are stored in base 2.  What the first attempt summed (reference 0) leaves with a power of two taken out, its sum in [1/2, 1): up to 2^64 of it times a value
+            // may be just finite here and not in the merge of several parts.  (With a running maximum the sum is at most 2^8 a key.)
+            const int e = m_run[qt] == 0.f ? __builtin_amdgcn_frexp_expf(l) : 0;         // (l = 0: 0)
+            const float out_of = __builtin_amdgcn_ldexpf(1.f, -e);
+            if (q4e == 0) *reinterpret_cast<f32x2*>(a.part + (size_t)a.total_q * a.q_heads * a.parts * D + at * 2) = f32x2{l == 0.f ? -__builtin_inff() : fmaf(m_run[qt], c, (float)e), l * out_of};
             if (l != 0.f) {                                  // (nothing to merge otherwise)
 #pragma unroll
-                for (int dt = 0; dt < DT; dt++) *reinterpret_cast<f32x4*>(a.part + at * D + dt * 16 + 4 * q4e) = o[dt][qt];
+                for (int dt = 0; dt < DT; dt++) *reinterpret_cast<f32x4*>(a.part + at * D + dt * 16 + 4 * q4e) = o[dt][qt] * out_of;
             }
             continue;
         }

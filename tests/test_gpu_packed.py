@@ -359,6 +359,33 @@ def test_attention_scores_far_from_zero(hb, dt, d, case, causal):
     assert rel_l2(got, want) < (4e-3 if dt == "bf16" else 1e-3)
 
 
+# (queries, keys, base-2 score that all pairs are near, exponent of the values): row blocks cut and not, single tokens
+SIZES = [([100], [3000], 50, 67), ([100], [3000], -60, -70), ([100], [3000], -20, -80), ([100, 3], [500, 90], -60, -70), ([100, 3], [500, 90], 60, 50), ([100, 3], [500, 90], 20, 90),
+         ([1, 1], [3000, 900], 50, 67), ([1, 1], [3000, 900], -60, -70)]
+
+
+@pytest.mark.parametrize("prescaled", [False, True])
+@pytest.mark.parametrize("case", SIZES, ids=[str(c).replace(" ", "") for c in SIZES])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_values_of_any_size(hb, dt, d, case, prescaled):
+    """Scores all far from zero on one side, and large or small values: what the softmax weighs is their mean, whatever the size of the numbers on the way.  (2^8 x keys x value stays below
+    2^128 in all of them.)"""
+    lq, lk, near, exponent = case
+
+    def edit(q, k, v, cu_q, cu_k):
+        # the first feature makes the common part of the score, a product of two numbers of at most 8 bits
+        q[..., 0] = 8.0 if near > 0 else -8.0
+        k[..., 0] = synth.round_bf16(np.float32(abs(near) / 8 * (1.0 if prescaled else d ** 0.5 / 1.4426950408889634)))
+        v[...] = np.abs(v) * np.float32(2.0 ** exponent)
+    got = _attention(hb, dt, lq, lk, 2, 1, d, prescaled=prescaled, edit=edit)
+    assert got[4] > 0 if max(lk) == 3000 else dt == "f32" or got[4] == 0
+    # (the common part in nats: sums of d products around it are off by up to 60 ln 2 x 2^-24 = 2.5e-6 a rounding, and a probability by as much; the bound has the worst case)
+    q, k, v, cu_q, cu_k, causal, factor = got[2]
+    bound = P.packed_attention_bound(q, k, v, cu_q, cu_k, dt == "bf16", causal, factor)
+    assert got[3] and np.isfinite(got[0]).all() and (np.abs(got[0] - got[1]) <= bound).all(), np.abs(got[0] / got[1] - 1).max()
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
