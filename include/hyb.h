@@ -364,7 +364,8 @@ typedef struct {
  * A query that sees no key (its sequence has none, or causal with n_q > n_k) or only scores of minus infinity gets zeros.  What a key holds that a query
  * does not see, infinities and NaN among it, does not reach that query.  Rows of o that belong to no sequence are left as they are.  o shares no element
  * with q, k or v; of these several may be one tensor, and strides of 0 are allowed.  Scores, the normaliser and the sums over values are fp32 (sums unnormalised: finite
- * while 2^8 times the number of keys times the largest value is below 2^128); bf16 rounds every probability once for its product with the values, and the result.
+ * while 2^8 times the number of keys times the largest value is below 2^128; at the other end they lose
+ * less than 2^-117 + 2^-94 times the largest value, times the number of keys); bf16 rounds every probability once for its product with the values, and the result.
  * Calls with few query rows cut the keys into parts that other workgroups take and merge the unnormalised partial results in a second kernel, in a
  * fixed order: deterministic, but the cut, which follows from the descriptor and the offsets alone, may decide last bits.
  * workspace: device, >= hyb_packed_attention_workspace_bytes(desc) (0: may be NULL), contents irrelevant; calls that overlap in time need one each. */

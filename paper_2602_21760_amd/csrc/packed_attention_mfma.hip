@@ -9,7 +9,9 @@
 // matter as long as both operands agree: k = 4 q4 + i of key tile 2 s, then of 2 s + 1).
 //
 // Softmax in fp32, base 2.  A workgroup first sums 2^(c score) without a reference maximum (c = scale x log2 e; 1 for queries that carry it);
-// that is the softmax as long as every row's sum lies in [2^-64, 2^64].  If a row's does not, the workgroup starts over with a running maximum.
+// that is the softmax as long as every row's sum lies in [2^-32, 2^64] and the sums over values are finite.  If a row's are not, the workgroup starts over with a running maximum.
+// (Products of a probability and a value below 2^-149 are lost: with a sum of 2^-32 a result is off by up to 2^-118 a key, with one of 2^-64 by 2^-86; and probabilities below 2^-126, which
+// is 2^-94 of such a sum.)
 // Probabilities are rounded to bf16 for the second contraction and the normaliser is the sum of the rounded ones.
 //
 // Masks: the last key that a row sees is one number per row (causal, or the end of the sequence); only tiles in which a wave's rows differ from
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
         for (int qt = 0; qt < 2; qt++) {
             const float l = row_total(l_run[qt]);
             // (a row that sees none of these keys has no sum to judge)
-            if (active && t_begin < t_end && row_last[wave * 32 + qt * 16 + lane_again() % 16] >= t_begin * BKV) out_of_range |= !(l > 0x1p-64f && l < 0x1p+64f);       // also true for NaN
+            if (active && t_begin < t_end && row_last[wave * 32 + qt * 16 + lane_again() % 16] >= t_begin * BKV) out_of_range |= !(l > 0x1p-32f && l < 0x1p+64f);       // also true for NaN
         }
         // an infinity or NaN in a row's result may come from a value that the row does not see (0 x it in an MFMA); 0 x the results finds them
         f32x4 zero = {0.f, 0.f, 0.f, 0.f};

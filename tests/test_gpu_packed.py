@@ -361,7 +361,7 @@ def test_attention_scores_far_from_zero(hb, dt, d, case, causal):
 
 # (queries, keys, base-2 score that all pairs are near, exponent of the values): row blocks cut and not, single tokens
 SIZES = [([100], [3000], 50, 67), ([100], [3000], -60, -70), ([100], [3000], -20, -80), ([100, 3], [500, 90], -60, -70), ([100, 3], [500, 90], 60, 50), ([100, 3], [500, 90], 20, 90),
-         ([1, 1], [3000, 900], 50, 67), ([1, 1], [3000, 900], -60, -70)]
+         ([1, 1], [3000, 900], 50, 67), ([1, 1], [3000, 900], -60, -70), ([100], [3000], -60, -92), ([100, 3], [500, 90], -60, -92), ([1, 1], [3000, 900], -60, -92)]
 
 
 @pytest.mark.parametrize("prescaled", [False, True])
@@ -370,7 +370,7 @@ SIZES = [([100], [3000], 50, 67), ([100], [3000], -60, -70), ([100], [3000], -20
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_values_of_any_size(hb, dt, d, case, prescaled):
     """Scores all far from zero on one side, and large or small values: what the softmax weighs is their mean, whatever the size of the numbers on the way.  (2^8 x keys x value stays below
-    2^128 in all of them.)"""
+    2^128 in all of them, and half a step of every result above 2^-117 x keys.)"""
     lq, lk, near, exponent = case
 
     def edit(q, k, v, cu_q, cu_k):
