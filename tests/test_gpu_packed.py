@@ -386,6 +386,27 @@ def test_attention_values_of_any_size(hb, dt, d, case, prescaled):
     assert got[3] and np.isfinite(got[0]).all() and (np.abs(got[0] - got[1]) <= bound).all(), np.abs(got[0] / got[1] - 1).max()
 
 
+@pytest.mark.parametrize("prescaled", [False, True])
+@pytest.mark.parametrize("factor", [12.0, 40.0])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_scores_far_from_zero_in_some_parts(hb, dt, d, factor, prescaled):
+    """Cut keys of which some parts need the running maximum and the others do not: references hundreds apart meet in the merge, in rows that weigh both kinds of parts and rows that weigh one."""
+    def edit(q, k, v, cu_q, cu_k):
+        k[1000:1500] *= np.float32(factor)
+        q[::2] *= np.float32(0.125)                        # these rows weigh all parts
+        q[5] = 0.0
+        if dt == "bf16":
+            for x in (q, k):
+                x[...] = synth.round_bf16(x)
+    got, want, inputs, same, need = _attention(hb, dt, [100], [3000], 2, 1, d, prescaled=prescaled, edit=edit)
+    assert need > 0 and same and np.isfinite(got).all()
+    q, k, v, cu_q, cu_k, causal, scale = inputs
+    assert (np.abs(got - want) <= P.packed_attention_bound(q, k, v, cu_q, cu_k, dt == "bf16", causal, scale)).all()
+    # (as for scores far from zero everywhere)
+    assert rel_l2(got, want) < (4e-3 if dt == "bf16" else 1e-3)
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
