@@ -3,8 +3,14 @@ aids under probes/ (one executable per source, next to it)."""
 import concurrent.futures as cf
 import glob
 import os
+import re
 import subprocess
 import sys
+
+if __package__:
+    from . import listing
+else:                       # run as a file
+    import listing
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -34,6 +40,27 @@ def _compile(src):
     return obj, r.stderr
 
 
+def has_asm(src):
+    """Inline asm with instructions in it (an empty statement or a wait alone needs no look at the listing)."""
+    with open(src) as f:
+        return re.search(r'asm[^;]*"[^"]*(ds_read|\bv_)', f.read()) is not None
+
+
+def listing_of(src):
+    """The compiler's listing of a source's kernels, as they are built."""
+    cmd = [_hipcc()] + HIPCC_FLAGS + ["--cuda-device-only", "-S", src, "-o", "-"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("hipcc failed for %s:\n%s" % (src, r.stderr))
+    return r.stdout
+
+
+def _check_listing(src):
+    found = listing.faults(listing_of(src))
+    if found:
+        raise RuntimeError("the code made from %s is not safe:\n%s" % (src, "\n".join(found)))
+
+
 def _probe(src):
     exe = src[:-4]
     cmd = [_hipcc()] + [f for f in HIPCC_FLAGS if f != "-fPIC"] + [src, "-o", exe]
@@ -51,6 +78,7 @@ def build(verbose=False, jobs=8):
     objs = []
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
         probes = [ex.submit(_probe, src) for src in sorted(glob.glob(os.path.join(PROBES, "*.hip")))]
+        checks = [ex.submit(_check_listing, src) for src in srcs if has_asm(src)]
         for fut in probes:
             _, err = fut.result()
             if verbose and err.strip():
@@ -59,6 +87,8 @@ def build(verbose=False, jobs=8):
             objs.append(obj)
             if verbose and err.strip():
                 sys.stderr.write(err)
+        for fut in checks:
+            fut.result()
     cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

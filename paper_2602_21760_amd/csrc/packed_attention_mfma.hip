@@ -49,7 +49,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // Transposing LDS reads of the V^T fragments of 32 output features (two 16-feature tiles, two 32-key steps of two reads each).  Written as asm so that they can be issued
 // ahead of their use: a wait that the compiler places before such a read through its builtin also waits for the next tile's copies.  Every result goes
-// through lds_wait(), which stands between these reads and their use and keeps the registers in use until they are written.
+// through lds_wait(), which stands between these reads and their use and keeps the registers in use until they are written.  (That nothing, a spill or a copy, touches the registers before is
+// looked up in the compiler's listing by the build.)
 template <int D, int PS>
 __device__ __forceinline__ void v_reads(unsigned at, bf16x4 (&vh)[2][PS][2]) {
     constexpr int ROWB = D * 2;
