@@ -355,7 +355,9 @@ __global__ __launch_bounds__(256, 4) void attention_mfma_kernel(AttnArgs a) {
                     for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)s[kt][qt][i];
         } else {
             // v_max3_f32 directly: fmaxf() makes the compiler canonicalise every MFMA output first (one extra
-            // multiply per score), which costs more than the maxima themselves
+            // multiply per score), which costs more than the maxima themselves.  A vector instruction may come 8 wait states after such an
+            // MFMA, which the compiler sees to for its own instructions but not for those in asm.
+            asm volatile("s_nop 7" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]), "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
             float mx[2];
 #pragma unroll
             for (int qt = 0; qt < 2; qt++) {

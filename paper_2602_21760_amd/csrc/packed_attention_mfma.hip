@@ -96,6 +96,13 @@ __device__ __forceinline__ void keep_order(V (&x)[N][2]) {
     for (int i = 0; i < N; i++) asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]));
 }
 
+// Stands between MFMAs and inline asm that takes their results: a vector instruction may come 8 wait states after a 16x16x32 MFMA, which the compiler sees to for its own instructions but
+// not for those in asm.
+__device__ __forceinline__ void mfma_wait(f32x4 (&x)[4][2]) {
+    asm volatile("s_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[1][0]), "+v"(x[1][1]), "+v"(x[2][0]), "+v"(x[2][1]), "+v"(x[3][0]), "+v"(x[3][1]));
+}
+__device__ __forceinline__ void mfma_wait(f32x4 (&x)[2][2]) { asm volatile("s_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[1][0]), "+v"(x[1][1])); }
+
 // The lane's index from an instruction the compiler cannot trace back: what rare paths and the epilogue derive from it is not kept in registers over the key loop.
 __device__ __forceinline__ int lane_again() {
     int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -271,6 +278,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
 #pragma unroll
                     for (int i = 0; i < 4; i++) pb[kt >> 1][qt][4 * (kt & 1) + i] = (bf16_t)s[kt][qt][i];
         } else {
+            mfma_wait(s);
             float mx[2];
 #pragma unroll
             for (int qt = 0; qt < 2; qt++) {

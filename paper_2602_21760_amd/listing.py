@@ -3,6 +3,8 @@
 For the compiler an LDS read written in asm has filled its registers when the statement ends; in truth the data arrives at a later wait.  The sources pass every such register
 through the statement that waits, so nothing that uses it can come earlier, but a copy, a spill or another value in the same register could.  Whether the code that was made has one
 depends on the compiler and on every edit, so build() looks.
+
+And a vector instruction that takes the result of an MFMA has to come some wait states behind it.  The compiler puts them before its own instructions, not before those in asm.
 """
 import re
 
@@ -84,5 +86,35 @@ def reads_in_flight(listing):
     return reads, sorted(faults)
 
 
+def mfma_wait_states(mfma):
+    """Wait states between an MFMA and a vector instruction that touches its result: the passes it takes (four rows of the result each, and in fp32 twice as many) and 4."""
+    if "_16x16x32_" in mfma:
+        return 8
+    return 12 if "_16x16x4_" in mfma else 20
+
+
+def early_uses_of_mfma_results(listing):
+    """[asm instructions that touch an MFMA's result too early]"""
+    found = set()
+    for name, code in _functions(listing).items():
+        labels = {label: i for i, (label, *_) in enumerate(code) if label is not None}
+        for i, (_, text, asm, line) in enumerate(code):
+            if text is None or not text.startswith("v_mfma"):
+                continue
+            need, result = mfma_wait_states(text), _registers(text.split(",")[0])
+
+            def stop(other, in_asm, at, states):
+                if states >= need:
+                    return True
+                # (what an LDS read fills arrives long after the MFMA's result)
+                used = other.split(",", 1)[-1] if other.startswith("ds_read") else other
+                if in_asm and other.startswith(("v_", "ds_")) and result & _registers(used):
+                    found.add("%s: '%s' (line %d) %d wait states after '%s' (line %d), not %d" % (name, other, at, states, text, line, need))
+                    return True
+                return False
+            _walk(code, labels, i, lambda other: int(other.split()[1], 0) + 1 if other.startswith("s_nop") else 1, stop)
+    return sorted(found)
+
+
 def faults(listing):
-    return reads_in_flight(listing)[1]
+    return reads_in_flight(listing)[1] + early_uses_of_mfma_results(listing)

@@ -38,6 +38,20 @@ def test_reads_in_flight(code, wrong):
     assert bool(listing.faults(_kernel(*code))) == wrong
 
 
+MFMA = "v_mfma_f32_16x16x32_bf16 v[4:7], v[8:11], v[12:15], v[4:7]"
+MAX = "asm: v_max3_f32 v0, v1, v2, v7"
+
+
+@pytest.mark.parametrize("code,wrong", [
+    ((MFMA, MAX), True), ((MFMA, "s_nop 6", MAX), True), ((MFMA, "s_nop 7", MAX), False), ((MFMA, "asm: s_nop 7", MAX), False), ((MFMA, "s_nop 3", "s_setprio 0", "v_mov_b32_e32 v20, 0", "s_nop 1", MAX), False),
+    ((MFMA, "asm: v_max3_f32 v0, v1, v2, v3", "asm: v_mov_b32 v4, 0"), True),                # written over
+    ((MFMA, "s_cbranch_scc0 .LBB0_2", "s_nop 7", ".LBB0_2:", MAX), True),                    # on one path
+    ((MFMA, "s_nop 0", "v_max3_f32 v0, v1, v2, v7"), False),                                 # the compiler's own
+    (("v_mfma_f32_16x16x4_f32 v[4:7], v8, v9, v[4:7]", "s_nop 7", MAX), True), (("v_mfma_f32_16x16x4_f32 v[4:7], v8, v9, v[4:7]", "s_nop 11", MAX), False)])
+def test_mfma_results(code, wrong):
+    assert bool(listing.faults(_kernel(*code))) == wrong
+
+
 def test_sources_with_asm_are_found():
     names = {os.path.basename(s) for s in SOURCES}
     assert {"packed_attention_mfma.hip", "packed_attention_few.hip", "attention_mfma.hip", "gemm_f32_mfma.hip"} <= names
