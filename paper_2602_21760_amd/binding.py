@@ -492,11 +492,11 @@ def hyb_packed_layout(shapes, offsets, request=None, positions=None, text_after=
 
 def _head_strides(t, name):
     """(token stride, head stride) of a [tokens, heads, head_dim] tensor whose features are adjacent, in elements; the stride of an axis of one element
-    says nothing and is taken as if the tensor were contiguous."""
+    says nothing and is taken as if the tensor were contiguous (a row of a head-major cache has heads far apart)."""
     if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
         raise ValueError("%s must be [tokens, heads, head_dim] with adjacent features" % name)
     head = t.stride(1) if t.shape[1] != 1 else t.shape[2]
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * head, t.shape[1] * t.shape[2]), head
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], head
 
 
 def _with_ints(tensors, *int_shapes):

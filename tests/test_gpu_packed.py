@@ -644,6 +644,16 @@ def test_attention_keys_beyond_32_bit_offsets(hb):
     assert rel_l2(host(o), P.packed_attention(host(q), host(k), host(v), [0, 1, 2], [0, 100, rows])) < 4e-3
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_one_row_of_head_major_caches(hb, dt):
+    """One token whose heads lie 2 MB apart, queries, keys, values and result: with one key the result is its value."""
+    q, k, v, o = (dev(synth.normal(s, (8, 8192, 128), 1.0, dt), tdt(dt))[:, s:s + 1].transpose(0, 1) for s in (1, 2, 3, 4))
+    cu = _offsets([1])
+    hb.hyb_packed_attention(hb.packed_attention_desc(q, k, v, o, cu, 1, 1), q, k, v, o, cu, cu)
+    # (p v / p: none of it rounds in bf16, three times in fp32)
+    assert (np.abs(host(o) - host(v)) <= (0.0 if dt == "bf16" else 3 * 2.0 ** -24) * np.abs(host(v))).all()
+
+
 def test_attention_binding_refusals(hb):
     q, k = (torch.zeros(8, h, 64, device="cuda", dtype=torch.bfloat16) for h in (2, 1))
     o, cu = torch.empty_like(q), _offsets([8])

@@ -193,3 +193,17 @@ def test_descriptors_from_tensors():
         hb.packed_attention_desc(q, k.float(), v, o, cu)
     one = torch.zeros(1, 4, 64).expand(1, 4, 64)
     assert hb._head_strides(one, "q") == (256, 64) and hb._head_strides(torch.zeros(5, 64)[:, None], "q") == (64, 64)
+
+
+def test_one_row_of_a_head_major_tensor(lib):
+    """The first step over an empty cache: heads far apart, one token, whose stride says nothing."""
+    import torch
+    from paper_2602_21760_amd import binding as hb
+    cache = torch.zeros(8, 8192, 128, dtype=torch.bfloat16)
+    cu = torch.tensor([0, 1], dtype=torch.int32)
+    for rows in (1, 2):
+        k = cache[:, :rows].transpose(0, 1)
+        d = hb.packed_attention_desc(k, k, k, k, cu)
+        assert (d.k_token_stride, d.k_head_stride) == (1024 if rows == 1 else 128, 8192 * 128)
+        # (the strides are accepted: what is missing is the first tensor)
+        assert lib.hyb_packed_attention(ctypes.byref(d), None, 4096, 4096, 4096, 4096, 4096, None, 0, None) == 1, lib.hyb_last_error_string()
