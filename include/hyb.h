@@ -347,7 +347,7 @@ typedef struct {
     int max_q, max_k;                                /* most queries / keys of one sequence, 0: unknown.  They choose the way to the result (single tokens want both), not the result */
     int q_heads, k_heads;                            /* q_heads % k_heads == 0: query head h reads key head h / (q_heads / k_heads) */
     int head_dim;                                    /* 64 or 128 */
-    float scale;                                     /* <= 0 means 1 / sqrt(head_dim) */
+    float scale;                                     /* <= 0 means 1 / sqrt(head_dim); scale * log2(e) must be finite */
     int causal;                                      /* non-zero: query i of a sequence of n_q queries and n_k keys sees the keys j <= i + n_k - n_q */
     int prescaled;                                   /* non-zero: q holds q * scale * log2(e) (as for hyb_joint_attention_prescaled); `scale` is not used */
     hyb_dtype dtype;

@@ -13,6 +13,8 @@
 // 32 rows at 128 (16 rows: 800, 300 and 1200 tokens, causal, 16 / 8 heads, 115 us, so 99; three sequences of 142 to 605, 4 heads: 25 and 34).  Ragged and small launches are held by the 10 us that a workgroup takes beside its tiles.
 #include "packed_attention.h"
 
+#include <math.h>
+
 namespace {
 
 constexpr int BKV = 32;
@@ -357,6 +359,7 @@ int fill_args(const char* who, const hyb_packed_attention_desc* desc, PackedAttn
     HYB_REQUIRE(d.sequences >= 0 && d.total_q >= 0 && d.total_k >= 0 && d.max_q >= 0 && d.max_k >= 0, HYB_ERR_SHAPE, "%s: negative size", who);
     HYB_REQUIRE(d.head_dim == 64 || d.head_dim == 128, HYB_ERR_SHAPE, "%s: head_dim %d is not supported (only 64 and 128)", who, d.head_dim);
     HYB_REQUIRE(d.q_heads > 0 && d.k_heads > 0 && d.q_heads <= 65535 && d.q_heads % d.k_heads == 0, HYB_ERR_SHAPE, "%s: %d query heads are no multiple of %d key heads", who, d.q_heads, d.k_heads);
+    HYB_REQUIRE(d.prescaled != 0 || d.scale <= 0.f || isfinite(d.scale * 1.4426950408889634f), HYB_ERR_SHAPE, "%s: scale %g is not finite in base 2", who, (double)d.scale);
     const size_t es = hyb_dtype_size(d.dtype), vec = 16 / es;
     const size_t strides[8] = {d.q_token_stride, d.q_head_stride, d.k_token_stride, d.k_head_stride, d.v_token_stride, d.v_head_stride, d.o_token_stride, d.o_head_stride};
     for (size_t s : strides) {

@@ -207,3 +207,12 @@ def test_one_row_of_a_head_major_tensor(lib):
         assert (d.k_token_stride, d.k_head_stride) == (1024 if rows == 1 else 128, 8192 * 128)
         # (the strides are accepted: what is missing is the first tensor)
         assert lib.hyb_packed_attention(ctypes.byref(d), None, 4096, 4096, 4096, 4096, 4096, None, 0, None) == 1, lib.hyb_last_error_string()
+
+
+@pytest.mark.parametrize("scale,code", [(float("nan"), 2), (float("inf"), 2), (3e38, 2), (2e38, 1), (1e-38, 1), (0.0, 1), (-1.0, 1), (float("-inf"), 1)])
+def test_attention_scale(lib, scale, code):
+    """A scale that is no number is refused, not taken for the default (accepted ones get as far as the missing tensor); one that is not used may be anything."""
+    from paper_2602_21760_amd import binding
+    call = lambda d: lib.hyb_packed_attention(ctypes.byref(d), None, 4096, 4096, 4096, 4096, 4096, None, 0, None)      # noqa: E731
+    assert call(_attention_desc(binding, scale=scale)) == code, lib.hyb_last_error_string()
+    assert call(_attention_desc(binding, scale=scale, prescaled=1)) == 1
