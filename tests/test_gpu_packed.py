@@ -534,6 +534,49 @@ def test_attention_offsets_outside_the_tensors(hb, dt):
             assert rel_l2(got, want) < TOL_REL[dt]
 
 
+def _guarded(x, fill, rows=64):
+    """(a tensor with x's data, whose neighbours in memory are rows of `fill`; a function that says whether they still are)"""
+    whole = torch.full((rows + x.shape[0] + rows, *x.shape[1:]), fill, device="cuda", dtype=x.dtype)
+    whole[rows:rows + x.shape[0]] = x
+    before = whole.clone()
+    bits = {torch.bfloat16: torch.int16, torch.float32: torch.int32, torch.uint8: torch.uint8}[x.dtype]
+
+    def intact():
+        return all(torch.equal(whole[part].view(bits), before[part].view(bits)) for part in (slice(0, rows), slice(rows + x.shape[0], None)))
+    return whole[rows:rows + x.shape[0]], intact
+
+
+# (rows of queries, rows of keys, max_q, max_k): uncut row blocks, cut ones, pieces of single tokens, and single tokens whose hints say one piece
+GUARDED = [(50, 50, 0, 0), (100, 3000, 100, 3000), (4, 3000, 1, 3000), (4, 3000, 1, 500)]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("case", GUARDED)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_offsets_outside_the_tensors_between_guards(hb, dt, d, case, causal):
+    """Offsets beyond the tensors, and offsets that decrease: NaN beside the inputs is not read, rows beside the result and bytes beside the workspace are not written."""
+    nq, nk, max_q, max_k = case
+    q, k, v = (synth.normal(s, (n, 2, d), 1.0, dt) for s, n in ((1, nq), (2, nk), (3, nk)))
+    (dq, q_ok), (dk, k_ok), (dv, v_ok) = (_guarded(dev(x, tdt(dt)), float("nan")) for x in (q, k, v))
+    for cu_q, cu_k in (([-3, 1, 2, 3, nq + 40], [-7, nk // 3, nk // 2, nk - 1, nk + 99999]), ([-2 ** 31, -1, nq // 2, 2 ** 31 - 1, 2 ** 31 - 1], [-2 ** 31, 0, nk // 2, 2 ** 31 - 1, 2 ** 31 - 1]),
+                       ([0, 1, 2, 3, 4], [nk - 9, nk // 30, nk, 5, nk // 2]), ([3, 1, 4, 0, 2], [0, nk // 4, nk // 2, nk // 2, nk]), ([nq, 3, 1, 1, -4], [nk + 5, nk // 2, 10, 8, -8])):
+        ordered = cu_q == sorted(cu_q) and cu_k == sorted(cu_k)
+        o, o_ok = _guarded(torch.full((nq, 2, d), 7.0, device="cuda", dtype=tdt(dt)), 9.0)
+        tq, tk = (torch.tensor(c, dtype=torch.int32).cuda() for c in (cu_q, cu_k))
+        desc = hb.packed_attention_desc(dq, dk, dv, o, tq, max_q, max_k, causal=causal)
+        # (numbers that decrease may leave parts of the workspace unwritten that are read)
+        ws, ws_ok = _guarded(torch.full((hb.hyb_packed_attention_workspace_bytes(desc),), 255 if ordered else 0, device="cuda", dtype=torch.uint8), 170, 4096)
+        hb.hyb_packed_attention(desc, dq, dk, dv, o, tq, tk, ws)
+        got = host(o)
+        assert q_ok() and k_ok() and v_ok() and o_ok() and ws_ok(), (cu_q, cu_k)
+        assert np.isfinite(got).all(), (cu_q, cu_k)
+        if ordered:
+            clip = [np.clip(c, 0, n) for c, n in ((cu_q, nq), (cu_k, nk))]
+            want = P.packed_attention(q, k, v, *clip, causal, None, np.full((nq, 2, d), 7.0))
+            assert (np.abs(got - want) <= P.packed_attention_bound(q, k, v, *clip, dt == "bf16", causal)).all(), (cu_q, cu_k)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_many_sequences(hb, dt):
     """More sequences than one step of the search looks at, empty ones among them."""
