@@ -577,6 +577,25 @@ def test_attention_offsets_outside_the_tensors_between_guards(hb, dt, d, case, c
             assert (np.abs(got - want) <= P.packed_attention_bound(q, k, v, *clip, dt == "bf16", causal)).all(), (cu_q, cu_k)
 
 
+@pytest.mark.parametrize("sequences", [5, 40])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_caches_with_room_to_grow(hb, dt, d, sequences):
+    """Single tokens over caches with spare rows: a sequence without queries owns the rows between two caches, whatever they hold."""
+    room, lens = 700, [1 + 173 * i % 700 for i in range(sequences)]
+
+    def edit(q, k, v, cu_q, cu_k):
+        for i, n in enumerate(lens):
+            k[i * room + n:(i + 1) * room] = np.nan
+            v[i * room + n:(i + 1) * room] = np.nan
+    lq, lk = [n for _ in lens for n in (1, 0)], [m for n in lens for m in (n, room - n)]
+    got, want, inputs, same, _ = _attention(hb, dt, lq, lk, 4, 2, d, causal=True, edit=edit)
+    q, k, v, cu_q, cu_k, causal, factor = inputs
+    bound = P.packed_attention_bound(q, np.nan_to_num(k), np.nan_to_num(v), cu_q, cu_k, dt == "bf16", causal, factor)
+    assert same and np.isfinite(got).all() and (np.abs(got - want) <= bound).all()
+    assert rel_l2(got, want) < TOL_REL[dt]
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_many_sequences(hb, dt):
     """More sequences than one step of the search looks at, empty ones among them."""
