@@ -5,8 +5,8 @@
 // S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: a 16-byte load gives a lane 4 features of its key for 4 MFMAs, and register i of the exponentiated S^T is the B operand of
 // the MFMA over the keys 4 q4 + i, with rows 4 q4 + i of V as the A operand.
 //
-// Bound by the matrix cores, which share their issue with everything else here: fp32 MFMAs and vector instructions of the waves of a SIMD do not overlap (busy 63 % and 24 % of the time
-// with 382 vector instructions beside the 128 MFMAs of a tile, no better with waves of different priority).  So a tile has few others: a probability is one fma and one
+// Bound by the matrix cores, which share their issue with everything else here: fp32 MFMAs and vector instructions of the waves of a SIMD do not overlap (busy 75 % and 22 % of the time
+// at head_dim 64, no better with waves of different priority).  So a tile has few others: a probability is one fma and one
 // v_exp_f32, 2^(c score - reference), whose error is that of an argument near 0 wherever the probability counts; masks, maxima across lanes and rescaling only where a tile asks for them;
 // offsets of buffer loads that no tile changes.  One sequence of 4096, 8 heads: head_dim 64 130 TFLOP/s, 128 118 (a large library product in fp32 reaches 139); with 16 rows 110 and 107.
 // The queries in LDS make room for a third workgroup at head_dim 64 (in registers, with the next tile's keys requested ahead: 314, 1302 and 259 tokens, 12 / 4 heads, 65 us, so 61) and for

@@ -1,10 +1,11 @@
 // Attention over packed batches for at most 16 rows a block (single new tokens, their heads of a group as rows), bf16, head_dim 64 or 128.
 //
-// Bound by memory: every key and value is read once, with 2 rows x 16 multiply-adds a byte at most (64 caches of 100 to 8000 keys, 8 heads of 128, 368 MB: 5.0 TB/s, and 5 us for the join; without
+// Bound by memory: every key and value is read once, with 8 multiply-adds a byte at most, one for each of 16 rows and 2 bytes (64 caches of 100 to 8000 keys, 8 heads of 128, 368 MB: 5.1 TB/s, and 5.6 us for the join; without
 // cuts, 215 caches of 3000: 5.6 TB/s).  So nothing is shared between waves: a workgroup of 4
 // waves owns the rows of one (sequence, key head) and a part of its keys, wave w takes the 32-key tiles w, w + 4, ... of it and streams them without a
 // barrier through an LDS tile of its own each for keys and values: the fragments of a tile go to registers at once, and the next tile's copy into the same
-// place is under way during this tile's arithmetic.  (Keys loaded straight to registers, 64 bytes of a row per instruction, reach 10 % less bandwidth.)  Running maximum and normaliser per wave; the four partial results are joined in LDS, in a
+// place is under way during this tile's arithmetic.  (Keys loaded straight to registers, 64 bytes of a row per instruction, reach 10 % less bandwidth.)  Running maximum and normaliser per wave, in fp32; probabilities are rounded to bf16 for the
+// product with the values, and the normaliser is the sum of the rounded ones, as where blocks have many rows; the four partial results are joined in LDS, in a
 // fixed order, and those of a sequence's parts by a second kernel.
 //
 // Caches are of all lengths, so workgroups are numbered by pieces of part_keys keys (as blocks of rows are elsewhere, see packed_find): a launch holds

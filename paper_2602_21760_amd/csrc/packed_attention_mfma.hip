@@ -12,10 +12,12 @@
 // that is the softmax as long as every row's sum lies in [2^-32, 2^64] and the sums over values are finite.  If a row's are not, the workgroup starts over with a running maximum.
 // (Products of a probability and a value below 2^-149 are lost: with a sum of 2^-32 a result is off by up to 2^-118 a key, with one of 2^-64 by 2^-86; and probabilities below 2^-126, which
 // is 2^-94 of such a sum.)
-// Probabilities are rounded to bf16 for the second contraction and the normaliser is the sum of the rounded ones.
+// Probabilities are rounded to bf16 for the second contraction, whose instruction takes both operands in one type (in fp32 it has a ninth of the rate), and the normaliser is the sum of the
+// rounded ones, so that a mean of equal values is that value.  This rounding is all that tells the results from rounded exact ones: 1.1e-3 to 1.6e-3 relative L2 before the results' own
+// rounding to bf16 (1.6e-3), 1.9e-3 to 2.3e-3 with it.
 //
 // Masks: the last key that a row sees is one number per row (causal, or the end of the sequence); only tiles in which a wave's rows differ from
-// "all 64" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA.  The first attempt lets them in; if a
+// "all of the tile" compare against it.  A probability of 0 does not keep an infinity or NaN of a hidden key's value out of an MFMA.  The first attempt lets them in; if a
 // result is not finite, the workgroup starts over in the same way as for sums out of range, and the second attempt searches every tile that not all rows see, zeroes such
 // values in the fragments and adds them to the rows that do see them.  (The search in the first attempt takes 3 to 9 % of launches over short sequences.)
 //
@@ -149,7 +151,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
 
     const int nt = (block_max + BKV) / BKV, part_tiles = packed_part_tiles(a, nt, BKV);        // (block_max == -1: no tile)
     const int t_begin = min(u.part * part_tiles, nt), t_end = min(t_begin + part_tiles, nt);
-    // Tiles t_begin .. plain_end - 1 are seen whole by all rows and followed by a tile of 64 keys: a loop of its own, which holds no masks in registers.
+    // Tiles t_begin .. plain_end - 1 are seen whole by all rows and followed by a whole tile of BKV keys: a loop of its own, which holds no masks in registers.
     const int block_min = packed_last_key(a, u, packed_div(u.row0, a.by_group));
     const int plain_end = min(min((block_min + 1) / BKV, u.n_k / BKV - 1), t_end - 1);
 
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void packed_attention_kernel(
     const int k_token = (int)a.k_token, v_token = (int)a.v_token;
     const int r0 = wave * CHUNK_ROWS + lane / SLOTS, slot_off = ((lane % SLOTS) ^ swz<D>(r0)) * 16;
     const int k_off = r0 * k_token + slot_off, v_off = r0 * v_token + slot_off;
-    auto issue = [&](int t, int buf, auto whole_tag) {     // whole: the tile has 64 keys
+    auto issue = [&](int t, int buf, auto whole_tag) {     // whole: the tile has BKV keys
         const int left = u.n_k - t * BKV;
         const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + (size_t)t * BKV * a.k_token), 0, (min(left, BKV) - 1) * k_token + ROWB, 0x00020000);
         const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + (size_t)t * BKV * a.v_token), 0, (min(left, BKV) - 1) * v_token + ROWB, 0x00020000);

@@ -167,9 +167,9 @@ int launch(RotaryArgs& a, bool halves, int q_heads, int k_heads, hipStream_t st)
     a.q_units = q_heads * a.head_units;
     a.units = (q_heads + k_heads) * a.head_units;
     // Tokens per workgroup: of those that make two to four units per thread the number that leaves the fewest threads without one in the last round, the smaller for
-    // the same (32 / 8 heads of 128, 65537 tokens: 512 units 200 us, 1024 203, 2048 206; 256 units 399: workgroups are then not started fast enough.  24 heads of
-    // 64 have 384 units a token: two tokens 6.3 us, one 7.2 where fp32 has 12 and 12); and few tokens spread over the chip (16 tokens of 32 / 8 heads of 128: one 2.8 us,
-    // three 3.9).
+    // the same (32 / 8 heads of 128, 65537 tokens: 512 units 200 us, 1024 203, 2048 206; 256 units 399: workgroups are then not started fast enough.  24 / 24
+    // heads of 64 have 384 units a token: 4429 tokens two at a time 10.9 us, one 11.7; 12 / 12 in fp32 as many: 2102 tokens 6.0 and 6.3); and few tokens spread over the chip (16 tokens of 32 / 8
+    // heads of 128: one a workgroup 3.2 us, two 3.8, three 4.3).  (Launches one after the other in a graph.)
     a.tile = 1;
     int best = 0;
     for (int t = 1; t <= 16 && (t == 1 || (t * a.units <= 4 * kThreads && t * 400 <= a.tokens)); t++) {      // (16 x 128 pairs, twice: 32 KB of LDS)
