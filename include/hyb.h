@@ -298,7 +298,7 @@ int hyb_mmdit_forward(const hyb_mmdit_desc* desc, const hyb_mmdit_weights* weigh
  * (sequence) s owns the rows offsets[s] .. offsets[s + 1] - 1; they do not decrease.  Offsets are read by the kernels only: a
  * captured graph replays on whatever they hold by then.  Offsets outside 0 .. the number of rows are taken as the nearest
  * of these, so that no call reads or writes outside its tensors.
- * Rows between two sequences (the spare room of caches that grow) are a sequence of their own, one without queries: what they hold is not looked at.
+ * Spare rows between two requests' keys (caches that grow) are described as a sequence without queries: what they hold is not looked at.
  * ---------------------------------------------------------------------------------------- */
 
 /* Offsets, request index and (time, height, width) position of every token of a packed batch from the requests' sizes.
